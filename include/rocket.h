@@ -262,6 +262,74 @@ int rocket_ridge_predict(const float* feat_dev, int N, int P, const float* w_dev
                          void* cuda_stream);
 
 /*
+ * What a trained head needs between the pooled features and the gradient of the kernels, and between that gradient and the
+ * optimiser (Sections 1 and 6: the soft PPV makes the kernels trainable): layer norm of the feature rows, forward and backward,
+ * and the norm of a gradient held in many tensors, with clipping.  Elements are fp32, binary16 or bfloat16, told apart by these
+ * codes; sums and statistics are fp32 or wider whatever the elements are, and every output is rounded once, from fp32.
+ * All calls run on the current device, only enqueue kernels, allocate nothing and may be captured into a CUDA graph.  Scratch
+ * memory is the caller's (workspace_dev, 16-byte aligned, contents arbitrary before and after): calls that may overlap on the
+ * device need one each.  Any tensor aligned to its element is accepted.
+ */
+#define ROCKET_F32 0
+#define ROCKET_F16 1
+#define ROCKET_BF16 2
+
+/*
+ * Layer norm of every row: with m = mean(x[n]) and v = mean((x[n] - m)^2),
+ *     y[n][p] = (x[n][p] - m) / sqrt(v + eps) * gamma[p] + beta[p].
+ *   x_dev     [N][P] of x_type, rows x_stride elements apart (0: one row for all N), values of a row next to one another
+ *   gamma_dev, beta_dev  [P] of w_type, either may be NULL (1 and 0)
+ *   y_dev     [N][P] of y_type, rows y_stride >= P elements apart, written; what lies between rows is not touched
+ *   mean_dev, rstd_dev   [N] fp32, written where not NULL: m and 1 / sqrt(v + eps), for the backward pass
+ * A row with a NaN or an infinity gives NaN in that row alone.  The strides count only with two rows and more.  N = 0 is a
+ * successful no-op.  ROCKET_EINVAL for a NULL or misaligned pointer, N < 0, P < 1, an unknown type, a negative or non-finite
+ * eps, and for an output that overlaps an input or another output (rows of two arrays may interleave at one byte distance).
+ */
+int rocket_layer_norm(const void* x_dev, int x_type, int64_t x_stride, int N, int P, const void* gamma_dev,
+                      const void* beta_dev, int w_type, float eps, void* y_dev, int y_type, int64_t y_stride,
+                      float* mean_dev, float* rstd_dev, void* cuda_stream);
+
+/*
+ * Backward of rocket_layer_norm: with xh = (x - mean) rstd and u = dy gamma,
+ *     dx[n][p]  = rstd[n] (u[n][p] - mean_p(u[n]) - xh[n][p] mean_p(u[n] xh[n]))
+ *     dgamma[p] = sum_n dy[n][p] xh[n][p]          dbeta[p] = sum_n dy[n][p]
+ *   dy_dev [N][P] of y_type, x_dev [N][P] of x_type, rows dy_stride and x_stride apart; gamma_dev as in the forward (NULL: 1);
+ *   mean_dev, rstd_dev from the forward
+ *   dx_dev [N][P] of x_type, rows dx_stride apart; dgamma_dev, dbeta_dev [P] of w_type; each assigned (not accumulated), or
+ *   left out where it is NULL (not all three)
+ *   workspace_dev  workspace_bytes >= rocket_layer_norm_backward_workspace(N, P) (which is ROCKET_EINVAL for sizes out of
+ *   range; 0 bytes may be NULL)
+ * The same call gives the same bits each time.  N = 0 writes zeros to dgamma and dbeta.  Errors as in the forward.
+ */
+int64_t rocket_layer_norm_backward_workspace(int N, int P);
+int rocket_layer_norm_backward(const void* dy_dev, int y_type, int64_t dy_stride, const void* x_dev, int x_type,
+                               int64_t x_stride, int N, int P, const void* gamma_dev, int w_type, const float* mean_dev,
+                               const float* rstd_dev, void* dx_dev, int64_t dx_stride, void* dgamma_dev, void* dbeta_dev,
+                               void* workspace_dev, int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The 2-norm of a gradient held in `count` tensors, and clipping by it:
+ *     norm = sqrt(sum over tensors and values of g^2)      c = min(1, max_norm / (norm + 1e-6))      out = c g
+ *   grads_dev, sizes, types  HOST arrays of `count` device pointers, element counts (0 allowed, its pointer is not used) and
+ *              type codes; read before the call returns
+ *   norm_dev   [1] fp32, written: the norm before clipping
+ *   out_dev, out_types  HOST arrays of the tensors that receive the clipped gradient, each of its gradient's type or fp32;
+ *              out_dev NULL: in place.  An entry may be its own gradient (of the same type)
+ *   workspace_dev  workspace_bytes >= rocket_grad_norm_workspace(count)
+ * Squares and sums are taken in double precision: no finite gradient overflows or vanishes in them.  The same call gives the
+ * same bits each time.  An infinite norm gives c = 0 (for max_norm finite), a NaN gives NaN everywhere; a caller that would
+ * rather skip such a step reads norm_dev.  ROCKET_EINVAL for a NULL or misaligned pointer, a negative count or size, an unknown or
+ * unfitting type, max_norm negative or NaN, and where anything written overlaps anything else (one tensor listed twice can be
+ * measured, not clipped).
+ */
+int64_t rocket_grad_norm_workspace(int count);
+int rocket_grad_norm(int count, const void* const* grads_dev, const int64_t* sizes, const int32_t* types, float* norm_dev,
+                     void* workspace_dev, int64_t workspace_bytes, void* cuda_stream);
+int rocket_clip_grad_norm(int count, const void* const* grads_dev, const int64_t* sizes, const int32_t* types,
+                          void* const* out_dev, const int32_t* out_types, float max_norm, float* norm_dev,
+                          void* workspace_dev, int64_t workspace_bytes, void* cuda_stream);
+
+/*
  * Replaces the weights and biases of the handle's kernels (host arrays laid out as
  * rocket_params_host_view returns them: n_weights ragged weights, K biases); lengths, dilations,
  * paddings and channels stay.  This is the step that makes the kernels trainable (the paper's

@@ -73,6 +73,19 @@ SIGNATURES = {
                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "rocket_ridge_predict": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                             ctypes.c_void_p, ctypes.c_void_p]),
+    "rocket_layer_norm": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_void_p, ctypes.c_int,
+                                         ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    "rocket_layer_norm_backward_workspace": (ctypes.c_int64, [ctypes.c_int, ctypes.c_int]),
+    "rocket_layer_norm_backward": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int,
+                                                  ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_int,
+                                                  ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+                                                  ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+                                                  ctypes.c_void_p]),
+    "rocket_grad_norm_workspace": (ctypes.c_int64, [ctypes.c_int]),
+    "rocket_grad_norm": (ctypes.c_int, [ctypes.c_int] + [ctypes.c_void_p] * 5 + [ctypes.c_int64, ctypes.c_void_p]),
+    "rocket_clip_grad_norm": (ctypes.c_int, [ctypes.c_int] + [ctypes.c_void_p] * 5 + [ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p,
+                                                                                      ctypes.c_int64, ctypes.c_void_p]),
     "rocket_transform_host": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
                                              ctypes.c_int, ctypes.c_void_p]),
     "rocket_transform_soft_host": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
@@ -407,6 +420,227 @@ def rocket_ridge_predict(feat, w, b, out=None):
                                                          _dev_ptr(b, f32, "b"), _dev_ptr(yhat, f32, "out"),
                                                          _current_stream()), "rocket_ridge_predict")
     return yhat
+
+
+_float_types = None
+
+
+def _types():
+    """{torch dtype: type code of include/rocket.h}."""
+    global _float_types
+    if _float_types is None:
+        torch = _t()
+        _float_types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+    return _float_types
+
+
+def _on_device(call, device, where):
+    """Runs call(stream) with `device` current, on that device's current stream."""
+    torch = _t()
+    if device.index == torch.cuda.current_device():
+        _check(call(_stream()), where)
+    else:
+        with torch.cuda.device(device):
+            _check(call(_stream()), where)
+
+
+def _rows(t, name, shape=None, device=None, dtype=None):
+    """(pointer, type code, row stride, N, P) of a CUDA tensor taken as rows of its last dimension: two dimensions with
+    any distance between the rows, or any number of contiguous ones."""
+    try:
+        code = _types().get(t.dtype)
+        if code is None or not t.is_cuda:
+            raise TypeError("%s must be a CUDA tensor of float32, float16 or bfloat16" % name)
+    except AttributeError:
+        raise TypeError("%s must be a CUDA tensor of float32, float16 or bfloat16" % name) from None
+    got = t.shape
+    if shape is not None and got != shape:
+        raise ValueError("%s must have the shape %s" % (name, tuple(shape)))
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError("%s must be of dtype %s" % (name, dtype))
+    if device is not None and t.device != device:
+        raise ValueError("%s is on another device" % name)
+    if len(got) == 2:
+        N, P = got
+        stride, step = t.stride()
+        if N > 1 and not t.is_contiguous():
+            if (P > 1 and step != 1) or stride < 0:
+                raise TypeError("%s must have the values of a row next to one another" % name)
+        elif P > 1 and step != 1:
+            raise TypeError("%s must have the values of a row next to one another" % name)
+        else:
+            stride = max(stride, P)
+    else:
+        if not got or not t.is_contiguous():
+            raise TypeError("%s must be contiguous, or have two dimensions" % name)
+        P = got[-1]
+        N, stride = t.numel() // P if P else 0, P
+    if P < 1 or N > 0x7fffffff or P > 0x7fffffff:
+        raise ValueError("%s must have rows of at least one value, and at most 2^31 - 1 rows and values per row" % name)
+    return t.data_ptr(), code, stride, N, P
+
+
+def _vector(t, n, name, device, dtype=None):
+    """(pointer, type code) of a contiguous CUDA tensor of n values, (None, None) of None."""
+    if t is None:
+        return None, None
+    try:
+        code = _types().get(t.dtype)
+        if code is None or not t.is_cuda or not t.is_contiguous() or (dtype is not None and t.dtype is not dtype):
+            raise TypeError("%s must be a contiguous CUDA tensor of dtype %s" % (name, dtype or "float32, float16 or bfloat16"))
+    except AttributeError:
+        raise TypeError("%s must be a tensor" % name) from None
+    if t.numel() != n or t.device != device:
+        raise ValueError("%s must hold %d values on the device of the rows" % (name, n))
+    return t.data_ptr(), code
+
+
+def rocket_layer_norm(feat, gamma=None, beta=None, eps=1e-5, out=None, out_dtype=None, mean_out=None, rstd_out=None, want_stats=True):
+    """Layer norm over the last dimension of feat (CUDA, float32 / float16 / bfloat16; [N, P] with any distance between the
+    rows, or contiguous): (feat - mean) * rstd * gamma + beta, in feat's type, out_dtype or out's.  gamma, beta: [P] of one
+    type, or None.  Returns (out, mean, rstd), the statistics fp32, one per row, or None without want_stats."""
+    torch = _t()
+    x, xt, xs, N, P = _rows(feat, "feat")
+    device = feat.device
+    y = out if out is not None else torch.empty(feat.shape, dtype=out_dtype or feat.dtype, device=device)
+    yp, yt, ys, _, _ = _rows(y, "out", feat.shape, device, out_dtype)
+    g, wt = _vector(gamma, P, "gamma", device)
+    b, bt = _vector(beta, P, "beta", device)
+    if wt is not None and bt is not None and wt != bt:
+        raise TypeError("gamma and beta must be of one dtype")
+    wt = wt if wt is not None else bt if bt is not None else 0
+    mean, rstd = mean_out, rstd_out
+    if want_stats:
+        lead = feat.shape[:-1]
+        if mean is None:
+            mean = torch.empty(lead, dtype=torch.float32, device=device)
+        if rstd is None:
+            rstd = torch.empty(lead, dtype=torch.float32, device=device)
+    mp, _ = _vector(mean, N, "mean_out", device, torch.float32)
+    rp, _ = _vector(rstd, N, "rstd_out", device, torch.float32)
+    fn = (_lib or load_library()).rocket_layer_norm
+    _on_device(lambda s: fn(x, xt, xs, N, P, g, b, wt, eps, yp, yt, ys, mp, rp, s), device, "rocket_layer_norm")
+    return y, mean, rstd
+
+
+def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dgamma_out=None, dbeta_out=None, want_dx=True,
+                               want_weights=True, weight_dtype=None):
+    """Gradients of sum(dy * rocket_layer_norm(feat)) for feat, gamma and beta, from the statistics of the forward pass.
+    Returns (dx of feat's type, dgamma, dbeta of gamma's type or weight_dtype); what is not wanted is None."""
+    torch = _t()
+    x, xt, xs, N, P = _rows(feat, "feat")
+    device = feat.device
+    d, yt, ds, _, _ = _rows(dy, "dy", feat.shape, device)
+    mp, _ = _vector(mean, N, "mean", device, torch.float32)
+    rp, _ = _vector(rstd, N, "rstd", device, torch.float32)
+    if mp is None or rp is None:
+        raise TypeError("mean and rstd must be the statistics of the forward pass")
+    g, wt = _vector(gamma, P, "gamma", device)
+    if weight_dtype is None:
+        weight_dtype = gamma.dtype if gamma is not None else dgamma_out.dtype if dgamma_out is not None else \
+            dbeta_out.dtype if dbeta_out is not None else torch.float32
+    elif gamma is not None and gamma.dtype is not weight_dtype:
+        raise TypeError("weight_dtype must be gamma's")
+    dx, dg, db = dx_out, dgamma_out, dbeta_out
+    if dx is None and want_dx:
+        dx = torch.empty(feat.shape, dtype=feat.dtype, device=device)
+    if want_weights:
+        if dg is None:
+            dg = torch.empty((P,), dtype=weight_dtype, device=device)
+        if db is None:
+            db = torch.empty((P,), dtype=weight_dtype, device=device)
+    dxp, dxs = None, 0
+    if dx is not None:
+        dxp, _, dxs, _, _ = _rows(dx, "dx_out", feat.shape, device, feat.dtype)
+    dgp, wt1 = _vector(dg, P, "dgamma_out", device, weight_dtype)
+    dbp, wt2 = _vector(db, P, "dbeta_out", device, weight_dtype)
+    wt = wt if wt is not None else wt1 if wt1 is not None else wt2 if wt2 is not None else 0
+    lib = _lib or load_library()
+    need = lib.rocket_layer_norm_backward_workspace(N, P)
+    ws = torch.empty((need,), dtype=torch.uint8, device=device) if need > 0 else None
+    wp = ws.data_ptr() if need > 0 else None
+    fn = lib.rocket_layer_norm_backward
+    _on_device(lambda s: fn(d, yt, ds, x, xt, xs, N, P, g, wt, mp, rp, dxp, dxs, dgp, dbp, wp, max(need, 0), s), device,
+               "rocket_layer_norm_backward")
+    return dx, dg, db
+
+
+def _dense(t):
+    """Whether the tensor's values fill a stretch of memory, in whatever order."""
+    if t.is_contiguous():
+        return True
+    n = 1
+    for stride, size in sorted(zip(t.stride(), t.shape)):
+        if size > 1:
+            if stride != n:
+                return False
+            n *= size
+    return True
+
+
+def _tensor_list(ts, name):
+    """(addresses, sizes, type codes) as arrays, and the device, of a sequence of CUDA tensors."""
+    types = _types()
+    n = len(ts)
+    ptrs, sizes, codes = (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
+    device = None
+    for i, t in enumerate(ts):
+        try:
+            code = types.get(t.dtype)
+            if code is None or not t.is_cuda or not _dense(t):
+                raise TypeError("%s must be dense CUDA tensors of float32, float16 or bfloat16" % name)
+        except AttributeError:
+            raise TypeError("%s must be a sequence of tensors" % name) from None
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError("%s must be on one device" % name)
+        ptrs[i], sizes[i], codes[i] = t.data_ptr(), t.numel(), code
+    return ptrs, sizes, codes, device
+
+
+def _norm_buffers(lib, count, device, norm_out):
+    torch = _t()
+    if device is None:
+        device = norm_out.device if norm_out is not None else torch.device("cuda", torch.cuda.current_device())
+    need = lib.rocket_grad_norm_workspace(count)
+    ws = torch.empty((need,), dtype=torch.uint8, device=device)
+    norm = norm_out if norm_out is not None else torch.empty((1,), dtype=torch.float32, device=device)
+    return device, ws, need, norm, _vector(norm, 1, "norm_out", device, torch.float32)[0]
+
+
+def rocket_grad_norm(grads, norm_out=None):
+    """2-norm of a gradient held in many tensors (a sequence of dense CUDA tensors of float32, float16 or bfloat16 on one
+    device).  Returns it as a [1] float32 tensor."""
+    lib = _lib or load_library()
+    ptrs, sizes, codes, device = _tensor_list(grads, "grads")
+    n = len(ptrs)
+    device, ws, need, norm, np_ = _norm_buffers(lib, n, device, norm_out)
+    wp = ws.data_ptr()
+    _on_device(lambda s: lib.rocket_grad_norm(n, ptrs, sizes, codes, np_, wp, need, s), device, "rocket_grad_norm")
+    return norm
+
+
+def rocket_clip_grad_norm(grads, max_norm, out=None, norm_out=None):
+    """Scales the gradient by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of out (each of its gradient's
+    shape and order of values, of its type or float32).  Returns (norm before clipping as a [1] float32 tensor, the clipped
+    tensors)."""
+    lib = _lib or load_library()
+    ptrs, sizes, codes, device = _tensor_list(grads, "grads")
+    n = len(ptrs)
+    op = oc = None
+    if out is not None:
+        op, osizes, oc, odevice = _tensor_list(out, "out")
+        if len(out) != n or odevice != device:
+            raise ValueError("out must hold one tensor per gradient, on the same device")
+        for a, b in zip(grads, out):
+            if a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())):
+                raise ValueError("out must have the shapes and strides of the gradients")
+    device, ws, need, norm, np_ = _norm_buffers(lib, n, device, norm_out)
+    wp = ws.data_ptr()
+    _on_device(lambda s: lib.rocket_clip_grad_norm(n, ptrs, sizes, codes, op, oc, max_norm, np_, wp, need, s), device,
+               "rocket_clip_grad_norm")
+    return norm, grads if out is None else out
 
 
 def _host_ptr(t, dtype, name):

@@ -1,0 +1,250 @@
+// Layer norm of rows, forward and backward: the step between pooled features and a trained head, and back.
+//
+//   m = mean(x)  v = mean((x - m)^2)  r = 1 / sqrt(v + eps)  y = (x - m) r g + b
+//   xh = (x - m) r  u = dy g  c1 = mean(u)  c2 = mean(u xh)  dx = r (u - c1 - xh c2)  dg = sum_n dy xh  db = sum_n dy
+//
+// Bound: memory (8 and 16 operations per value).
+#include <cooperative_groups.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "rocket_float_types.cuh"
+#include "rocket_internal.h"
+
+namespace rocket {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+
+struct Pair { double a, b; };
+
+// Sums of two values over the block, in a fixed order; every thread gets them.
+__device__ __forceinline__ Pair block_sums(double a, double b) {
+    __shared__ double red[2][kWarps];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) { red[0][threadIdx.x >> 5] = a; red[1][threadIdx.x >> 5] = b; }
+    __syncthreads();
+    a = b = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) { a += red[0][w]; b += red[1][w]; }
+    return {a, b};
+}
+
+// A block per row, the row read three times.  The variance is taken about the mean as rounded to fp32, and the rest of the
+// mean that this leaves is taken off both: rows far from zero lose nothing that fp32 holds.
+template <class TX, class TY, class TW>
+__global__ void __launch_bounds__(kThreads)
+norm_rows_kernel(const TX* __restrict__ x, int64_t x_stride, int N, int P, const TW* __restrict__ gamma,
+                 const TW* __restrict__ beta, float eps, TY* __restrict__ y, int64_t y_stride, float* __restrict__ mean,
+                 float* __restrict__ rstd) {
+    for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
+        const TX* __restrict__ row = x + n * x_stride;
+        double s = 0.0, q = 0.0;
+        for (int64_t i = threadIdx.x; i < P; i += kThreads) s += (double)to_float(row[i]);
+        const double total = block_sums(s, 0.0).a;
+        const float m = (float)(total / (double)P);
+        s = 0.0;
+        for (int64_t i = threadIdx.x; i < P; i += kThreads) {
+            const double d = (double)(to_float(row[i]) - m);
+            s += d;
+            q += d * d;
+        }
+        const Pair t = block_sums(s, q);
+        const double rest = t.a / (double)P;
+        const float r = (float)(1.0 / sqrt(fmax(t.b / (double)P - rest * rest, 0.0) + (double)eps));
+        for (int64_t i = threadIdx.x; i < P; i += kThreads) {
+            float v = ((to_float(row[i]) - m) - (float)rest) * r;
+            if (gamma) v *= to_float(gamma[i]);
+            if (beta) v += to_float(beta[i]);
+            y[n * y_stride + i] = from_float<TY>(v);
+        }
+        if (threadIdx.x == 0) {
+            if (mean) mean[n] = (float)((double)m + rest);
+            if (rstd) rstd[n] = r;
+        }
+    }
+}
+
+template <class TX, class TY, class TW>
+__global__ void __launch_bounds__(kThreads)
+norm_backward_rows_kernel(const TY* __restrict__ dy, int64_t dy_stride, const TX* __restrict__ x, int64_t x_stride, int N,
+                          int P, const TW* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
+                          TX* __restrict__ dx, int64_t dx_stride) {
+    for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
+        const float m = mean[n], r = rstd[n];
+        double s = 0.0, q = 0.0;
+        for (int64_t i = threadIdx.x; i < P; i += kThreads) {
+            const float u = to_float(dy[n * dy_stride + i]) * (gamma ? to_float(gamma[i]) : 1.0f);
+            const float xh = (to_float(x[n * x_stride + i]) - m) * r;
+            s += (double)u;
+            q += (double)u * (double)xh;
+        }
+        const Pair t = block_sums(s, q);
+        const float c1 = (float)(t.a / (double)P), c2 = (float)(t.b / (double)P);
+        for (int64_t i = threadIdx.x; i < P; i += kThreads) {
+            const float u = to_float(dy[n * dy_stride + i]) * (gamma ? to_float(gamma[i]) : 1.0f);
+            const float xh = (to_float(x[n * x_stride + i]) - m) * r;
+            dx[n * dx_stride + i] = from_float<TX>(r * (u - c1 - xh * c2));
+        }
+    }
+}
+
+// A block owns 32 columns, its warps share the rows.
+template <class TX, class TY, class TW>
+__global__ void __launch_bounds__(kThreads)
+norm_weight_grads_kernel(const TY* __restrict__ dy, int64_t dy_stride, const TX* __restrict__ x, int64_t x_stride, int N,
+                         int P, const float* __restrict__ mean, const float* __restrict__ rstd, TW* __restrict__ dgamma,
+                         TW* __restrict__ dbeta) {
+    __shared__ double red[2][kWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t p = (int64_t)blockIdx.x * 32 + lane;
+    double s = 0.0, q = 0.0;
+    if (p < P)
+        for (int64_t n = warp; n < N; n += kWarps) {
+            const float d = to_float(dy[n * dy_stride + p]);
+            const float xh = (to_float(x[n * x_stride + p]) - mean[n]) * rstd[n];
+            s += (double)d;
+            q += (double)d * (double)xh;
+        }
+    red[0][warp][lane] = s;
+    red[1][warp][lane] = q;
+    __syncthreads();
+    if (warp == 0 && p < P) {
+        s = q = 0.0;
+        for (int w = 0; w < kWarps; ++w) { s += red[0][w][lane]; q += red[1][w][lane]; }
+        if (dgamma) dgamma[p] = from_float<TW>((float)q);
+        if (dbeta) dbeta[p] = from_float<TW>((float)s);
+    }
+}
+
+// Rows [N][P] of `bytes` bytes a value, `stride` values apart.
+struct Rows {
+    uintptr_t base;
+    int64_t N, P, stride;
+    int bytes;
+    uintptr_t end() const { return base + (uintptr_t)((N - 1) * stride + P) * bytes; }
+};
+
+// Whether an output shares a byte with another array.  Rows of equal distance may interleave (halves of one wider buffer).
+bool overlap(const Rows& a, const Rows& b) {
+    if (!a.base || !b.base || a.end() <= b.base || b.end() <= a.base) return false;
+    const uintptr_t step = (uintptr_t)a.stride * a.bytes;
+    if (a.N > 1 && step == (uintptr_t)b.stride * b.bytes && step > 0) {
+        const uintptr_t wa = (uintptr_t)a.P * a.bytes, wb = (uintptr_t)b.P * b.bytes;
+        const uintptr_t off = b.base >= a.base ? (b.base - a.base) % step : (step - (a.base - b.base) % step) % step;
+        return !(off >= wa && off + wb <= step);
+    }
+    return true;
+}
+
+bool misaligned(const void* p, int type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(float_type_bytes(type) - 1)) != 0; }
+
+int status_of(cudaError_t e) {
+    if (e == cudaSuccess) return ROCKET_OK;
+    cudaGetLastError();
+    return e == cudaErrorMemoryAllocation ? ROCKET_ENOMEM : ROCKET_ECUDA;
+}
+
+// Strides whose byte offsets stay far inside 64 bits; the rows of an output do not overlap.
+bool stride_ok(int N, int P, int64_t stride, bool output) {
+    return N <= 1 || (stride >= (output ? P : 0) && stride <= (int64_t(1) << 58) / N);
+}
+
+}  // namespace
+}  // namespace rocket
+
+using namespace rocket;
+
+extern "C" int rocket_layer_norm(const void* x_dev, int x_type, int64_t x_stride, int N, int P, const void* gamma_dev,
+                                 const void* beta_dev, int w_type, float eps, void* y_dev, int y_type, int64_t y_stride,
+                                 float* mean_dev, float* rstd_dev, void* cuda_stream) {
+    if (!is_float_type(x_type) || !is_float_type(y_type) || !is_float_type(w_type)) return ROCKET_EINVAL;
+    if (N < 0 || P < 1 || !(eps >= 0.0f) || std::isinf(eps)) return ROCKET_EINVAL;
+    if (N == 0) return ROCKET_OK;
+    if (!x_dev || !y_dev || !stride_ok(N, P, x_stride, false) || !stride_ok(N, P, y_stride, true)) return ROCKET_EINVAL;
+    if (misaligned(x_dev, x_type) || misaligned(y_dev, y_type) || misaligned(gamma_dev, w_type) || misaligned(beta_dev, w_type) ||
+        misaligned(mean_dev, ROCKET_F32) || misaligned(rstd_dev, ROCKET_F32))
+        return ROCKET_EINVAL;
+    const Rows in[] = {{(uintptr_t)x_dev, N, P, N > 1 ? x_stride : P, float_type_bytes(x_type)},
+                       {(uintptr_t)gamma_dev, 1, P, P, float_type_bytes(w_type)},
+                       {(uintptr_t)beta_dev, 1, P, P, float_type_bytes(w_type)}};
+    const Rows out[] = {{(uintptr_t)y_dev, N, P, N > 1 ? y_stride : P, float_type_bytes(y_type)},
+                        {(uintptr_t)mean_dev, 1, N, N, 4},
+                        {(uintptr_t)rstd_dev, 1, N, N, 4}};
+    for (int o = 0; o < 3; ++o) {
+        for (const Rows& i : in) if (overlap(out[o], i)) return ROCKET_EINVAL;
+        for (int p = 0; p < o; ++p) if (overlap(out[o], out[p])) return ROCKET_EINVAL;
+    }
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const unsigned blocks = (unsigned)std::min(N, 148 * 8);
+    with_float_type(x_type, [&](auto* tx) {
+        with_float_type(y_type, [&](auto* ty) {
+            with_float_type(w_type, [&](auto* tw) {
+                norm_rows_kernel<<<blocks, kThreads, 0, stream>>>((decltype(tx))x_dev, x_stride, N, P, (decltype(tw))gamma_dev,
+                                                                  (decltype(tw))beta_dev, eps, (decltype(ty))y_dev, y_stride, mean_dev, rstd_dev);
+            });
+        });
+    });
+    count_launch();
+    return status_of(cudaGetLastError());
+}
+
+extern "C" int64_t rocket_layer_norm_backward_workspace(int N, int P) {
+    return N < 0 || P < 1 ? ROCKET_EINVAL : 0;
+}
+
+extern "C" int rocket_layer_norm_backward(const void* dy_dev, int y_type, int64_t dy_stride, const void* x_dev, int x_type,
+                                          int64_t x_stride, int N, int P, const void* gamma_dev, int w_type,
+                                          const float* mean_dev, const float* rstd_dev, void* dx_dev, int64_t dx_stride,
+                                          void* dgamma_dev, void* dbeta_dev, void* workspace_dev, int64_t workspace_bytes,
+                                          void* cuda_stream) {
+    if (!is_float_type(x_type) || !is_float_type(y_type) || !is_float_type(w_type)) return ROCKET_EINVAL;
+    if (N < 0 || P < 1 || workspace_bytes < 0 || (!dx_dev && !dgamma_dev && !dbeta_dev)) return ROCKET_EINVAL;
+    if (misaligned(dgamma_dev, w_type) || misaligned(dbeta_dev, w_type) || misaligned(gamma_dev, w_type) || misaligned(dy_dev, y_type) ||
+        misaligned(x_dev, x_type) || misaligned(dx_dev, x_type) || misaligned(mean_dev, ROCKET_F32) || misaligned(rstd_dev, ROCKET_F32))
+        return ROCKET_EINVAL;
+    if (N > 0 && (!dy_dev || !x_dev || !mean_dev || !rstd_dev)) return ROCKET_EINVAL;
+    if (!stride_ok(N, P, dy_stride, false) || !stride_ok(N, P, x_stride, false) || (dx_dev && !stride_ok(N, P, dx_stride, true))) return ROCKET_EINVAL;
+    const int64_t need = rocket_layer_norm_backward_workspace(N, P);
+    if (workspace_bytes < need || (need > 0 && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15u)))) return ROCKET_EINVAL;
+    const int xb = float_type_bytes(x_type), wb = float_type_bytes(w_type);
+    const Rows none = {0, 1, 1, 1, 1};
+    const Rows in[] = {N ? Rows{(uintptr_t)dy_dev, N, P, N > 1 ? dy_stride : P, float_type_bytes(y_type)} : none,
+                       N ? Rows{(uintptr_t)x_dev, N, P, N > 1 ? x_stride : P, xb} : none,
+                       {(uintptr_t)gamma_dev, 1, P, P, wb},
+                       N ? Rows{(uintptr_t)mean_dev, 1, N, N, 4} : none,
+                       N ? Rows{(uintptr_t)rstd_dev, 1, N, N, 4} : none};
+    const Rows out[] = {N ? Rows{(uintptr_t)dx_dev, N, P, N > 1 ? dx_stride : P, xb} : none,
+                        {(uintptr_t)dgamma_dev, 1, P, P, wb},
+                        {(uintptr_t)dbeta_dev, 1, P, P, wb},
+                        need ? Rows{(uintptr_t)workspace_dev, 1, need, need, 1} : none};
+    for (int o = 0; o < 4; ++o) {
+        for (const Rows& i : in) if (overlap(out[o], i)) return ROCKET_EINVAL;
+        for (int p = 0; p < o; ++p) if (overlap(out[o], out[p])) return ROCKET_EINVAL;
+    }
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const unsigned blocks = (unsigned)std::min(N, 148 * 8);
+    with_float_type(x_type, [&](auto* tx) {
+        with_float_type(y_type, [&](auto* ty) {
+            with_float_type(w_type, [&](auto* tw) {
+                if (dx_dev && N > 0) {
+                    norm_backward_rows_kernel<<<blocks, kThreads, 0, stream>>>((decltype(ty))dy_dev, dy_stride, (decltype(tx))x_dev, x_stride, N, P,
+                                                                               (decltype(tw))gamma_dev, mean_dev, rstd_dev, (decltype(tx))dx_dev, dx_stride);
+                    count_launch();
+                }
+                if (dgamma_dev || dbeta_dev) {
+                    norm_weight_grads_kernel<<<(unsigned)(((int64_t)P + 31) / 32), kThreads, 0, stream>>>((decltype(ty))dy_dev, dy_stride, (decltype(tx))x_dev, x_stride, N, P,
+                                                                                                 mean_dev, rstd_dev, (decltype(tw))dgamma_dev, (decltype(tw))dbeta_dev);
+                    count_launch();
+                }
+            });
+        });
+    });
+    return status_of(cudaGetLastError());
+}
