@@ -11,6 +11,7 @@
 
 #include "rocket_float_types.cuh"
 #include "rocket_internal.h"
+#include "rocket_norm.h"
 
 namespace rocket {
 namespace {
@@ -34,41 +35,6 @@ __device__ __forceinline__ Pair block_sums(double a, double b) {
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) { a += red[0][w]; b += red[1][w]; }
     return {a, b};
-}
-
-// A block per row, the row read three times.  The variance is taken about the mean as rounded to fp32, and the rest of the
-// mean that this leaves is taken off both: rows far from zero lose nothing that fp32 holds.
-template <class TX, class TY, class TW>
-__global__ void __launch_bounds__(kThreads)
-norm_rows_kernel(const TX* __restrict__ x, int64_t x_stride, int N, int P, const TW* __restrict__ gamma,
-                 const TW* __restrict__ beta, float eps, TY* __restrict__ y, int64_t y_stride, float* __restrict__ mean,
-                 float* __restrict__ rstd) {
-    for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
-        const TX* __restrict__ row = x + n * x_stride;
-        double s = 0.0, q = 0.0;
-        for (int64_t i = threadIdx.x; i < P; i += kThreads) s += (double)to_float(row[i]);
-        const double total = block_sums(s, 0.0).a;
-        const float m = (float)(total / (double)P);
-        s = 0.0;
-        for (int64_t i = threadIdx.x; i < P; i += kThreads) {
-            const double d = (double)(to_float(row[i]) - m);
-            s += d;
-            q += d * d;
-        }
-        const Pair t = block_sums(s, q);
-        const double rest = t.a / (double)P;
-        const float r = (float)(1.0 / sqrt(fmax(t.b / (double)P - rest * rest, 0.0) + (double)eps));
-        for (int64_t i = threadIdx.x; i < P; i += kThreads) {
-            float v = ((to_float(row[i]) - m) - (float)rest) * r;
-            if (gamma) v *= to_float(gamma[i]);
-            if (beta) v += to_float(beta[i]);
-            y[n * y_stride + i] = from_float<TY>(v);
-        }
-        if (threadIdx.x == 0) {
-            if (mean) mean[n] = (float)((double)m + rest);
-            if (rstd) rstd[n] = r;
-        }
-    }
 }
 
 template <class TX, class TY, class TW>
@@ -182,17 +148,8 @@ extern "C" int rocket_layer_norm(const void* x_dev, int x_type, int64_t x_stride
         for (int p = 0; p < o; ++p) if (overlap(out[o], out[p])) return ROCKET_EINVAL;
     }
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const unsigned blocks = (unsigned)std::min(N, 148 * 8);
-    with_float_type(x_type, [&](auto* tx) {
-        with_float_type(y_type, [&](auto* ty) {
-            with_float_type(w_type, [&](auto* tw) {
-                norm_rows_kernel<<<blocks, kThreads, 0, stream>>>((decltype(tx))x_dev, x_stride, N, P, (decltype(tw))gamma_dev,
-                                                                  (decltype(tw))beta_dev, eps, (decltype(ty))y_dev, y_stride, mean_dev, rstd_dev);
-            });
-        });
-    });
-    count_launch();
-    return status_of(cudaGetLastError());
+    const norm::Forward a = {x_dev, y_dev, gamma_dev, beta_dev, mean_dev, rstd_dev, x_stride, y_stride, N, P, x_type, y_type, w_type, eps};
+    return status_of(norm::launch_forward(a, stream));
 }
 
 extern "C" int64_t rocket_layer_norm_backward_workspace(int N, int P) {
