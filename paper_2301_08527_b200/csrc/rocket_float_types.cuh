@@ -30,41 +30,102 @@ auto with_float_type(int type, F&& f) {
     return type == ROCKET_F32 ? f((float*)nullptr) : type == ROCKET_F16 ? f((__half*)nullptr) : f((__nv_bfloat16*)nullptr);
 }
 
-// W values of T that lie next to one another, as they are in memory: loaded and stored in words of up to 16 bytes, which the
-// address has to be a multiple of (W = 1: any element's).
+// W values of T that lie next to one another, as the words of up to 16 bytes they are loaded and stored in (addresses are multiples
+// of a word's size).
 template <class T, int W>
-struct alignas(sizeof(T) * W < 16 ? sizeof(T) * W : 16) Packed {
-    T v[W];
+struct Packed {
+    static constexpr int kBytes = (int)sizeof(T) * W, kWord = kBytes < 16 ? kBytes : 16, kWords = kBytes / kWord;
+    using Word = std::conditional_t<kWord == 16, uint4, std::conditional_t<kWord == 8, uint2, std::conditional_t<kWord == 4, unsigned, unsigned short>>>;
+    Word w[kWords];
+    __device__ __forceinline__ T get(int i) const { return reinterpret_cast<const T*>(w)[i]; }
+    __device__ __forceinline__ uint32_t pair(int i) const { return reinterpret_cast<const uint32_t*>(w)[i]; }
 };
 
 template <class T, int W>
-__device__ __forceinline__ Packed<T, W> load_packed(const T* p) { return *reinterpret_cast<const Packed<T, W>*>(p); }
+__device__ __forceinline__ Packed<T, W> load_packed(const T* p) {
+    using P = Packed<T, W>;
+    P r;
+#pragma unroll
+    for (int i = 0; i < P::kWords; ++i) r.w[i] = reinterpret_cast<const typename P::Word*>(p)[i];
+    return r;
+}
 
 // The same for data that no thread writes while the kernel runs.
 template <class T, int W>
 __device__ __forceinline__ Packed<T, W> load_packed_ro(const T* p) {
-    constexpr int bytes = (int)sizeof(T) * W;
-    Packed<T, W> r;
-    if constexpr (bytes % 16 == 0) {
+    using P = Packed<T, W>;
+    P r;
 #pragma unroll
-        for (int i = 0; i < bytes / 16; ++i) reinterpret_cast<uint4*>(&r)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
-    } else if constexpr (bytes == 8) {
-        *reinterpret_cast<uint2*>(&r) = __ldg(reinterpret_cast<const uint2*>(p));
-    } else if constexpr (bytes == 4) {
-        *reinterpret_cast<uint32_t*>(&r) = __ldg(reinterpret_cast<const unsigned*>(p));
+    for (int i = 0; i < P::kWords; ++i) r.w[i] = __ldg(reinterpret_cast<const typename P::Word*>(p) + i);
+    return r;
+}
+
+// The values as fp32, 16-bit ones in pairs from the words that hold them.
+template <class T, int W>
+__device__ __forceinline__ void unpack(const Packed<T, W>& r, float (&v)[W]) {
+    if constexpr (sizeof(T) == 2 && W % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) {
+            const uint32_t w = r.pair(i);
+            if constexpr (std::is_same_v<T, __half>) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+                v[2 * i] = f.x;
+                v[2 * i + 1] = f.y;
+            } else {                       // a bfloat16 is the upper half of the fp32 value
+                v[2 * i] = __uint_as_float(w << 16);
+                v[2 * i + 1] = __uint_as_float(w & 0xffff0000u);
+            }
+        }
     } else {
-        static_assert(bytes == 2, "");
-        *reinterpret_cast<uint16_t*>(&r) = __ldg(reinterpret_cast<const unsigned short*>(p));
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = to_float(r.get(i));
+    }
+}
+
+// The same for data that is read once: it takes no place in L1, which is left to what is read again.
+template <class T, int W>
+__device__ __forceinline__ Packed<T, W> load_packed_once(const T* p) {
+    using P = Packed<T, W>;
+    P r;
+    if constexpr (P::kWord == 16) {
+#pragma unroll
+        for (int i = 0; i < P::kWords; ++i)
+            asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w) : "l"(reinterpret_cast<const uint4*>(p) + i));
+    } else if constexpr (P::kWord == 8) {
+        asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.w[0].x), "=r"(r.w[0].y) : "l"(p));
+    } else {
+        r = load_packed_ro<T, W>(p);
     }
     return r;
 }
 
 template <class T, int W>
 __device__ __forceinline__ void store_packed(T* p, const float (&v)[W]) {
-    Packed<T, W> r;
+    using P = Packed<T, W>;
+    P r;
+    if constexpr (sizeof(T) == 2 && W % 2 == 0) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) r.v[i] = from_float<T>(v[i]);
-    *reinterpret_cast<Packed<T, W>*>(p) = r;
+        for (int i = 0; i < W / 2; ++i) {
+            uint32_t& w = reinterpret_cast<uint32_t*>(r.w)[i];
+            if constexpr (std::is_same_v<T, __half>) {
+                const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+                w = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                w = *reinterpret_cast<const uint32_t*>(&h);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const T t = from_float<T>(v[i]);
+            if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(r.w)[i] = __float_as_uint(t);
+            else reinterpret_cast<unsigned short*>(r.w)[i] = *reinterpret_cast<const unsigned short*>(&t);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < P::kWords; ++i) reinterpret_cast<typename P::Word*>(p)[i] = r.w[i];
 }
 
 // Values `i` to `i` + W - 1 of an array whose type is known at run time only (the branch is the same for all threads).
@@ -72,9 +133,7 @@ template <int W>
 __device__ __forceinline__ void load_typed(const void* p, int type, int64_t i, float (&v)[W]) {
     auto get = [&](auto* t) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(t)>>;
-        const Packed<T, W> r = load_packed_ro<T, W>(t + i);
-#pragma unroll
-        for (int k = 0; k < W; ++k) v[k] = to_float(r.v[k]);
+        unpack<T, W>(load_packed_ro<T, W>(t + i), v);
     };
     if (type == ROCKET_F32) get(static_cast<const float*>(p));
     else if (type == ROCKET_F16) get(static_cast<const __half*>(p));
