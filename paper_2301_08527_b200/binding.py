@@ -556,7 +556,7 @@ def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dg
     dbp, wt2 = _vector(db, P, "dbeta_out", device, weight_dtype)
     wt = wt if wt is not None else wt1 if wt1 is not None else wt2 if wt2 is not None else 0
     lib = _lib or load_library()
-    need = lib.rocket_layer_norm_backward_workspace(N, P)
+    need = lib.rocket_layer_norm_backward_workspace(N, P) if dg is not None or db is not None else 0
     ws = torch.empty((need,), dtype=torch.uint8, device=device) if need > 0 else None
     wp = ws.data_ptr() if need > 0 else None
     fn = lib.rocket_layer_norm_backward

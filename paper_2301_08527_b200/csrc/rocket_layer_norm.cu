@@ -1,12 +1,5 @@
-// Layer norm of rows, forward and backward: the step between pooled features and a trained head, and back.
-//
-//   m = mean(x)  v = mean((x - m)^2)  r = 1 / sqrt(v + eps)  y = (x - m) r g + b
-//   xh = (x - m) r  u = dy g  c1 = mean(u)  c2 = mean(u xh)  dx = r (u - c1 - xh c2)  dg = sum_n dy xh  db = sum_n dy
-//
-// Bound: memory (8 and 16 operations per value).
-#include <cooperative_groups.h>
-
-#include <algorithm>
+// Layer norm of rows, forward and backward: the step between pooled features and a trained head, and back.  The entry points and
+// their checks; the kernels are in rocket_norm_forward.cu and rocket_norm_backward.cu.
 #include <cmath>
 
 #include "rocket_float_types.cuh"
@@ -15,79 +8,6 @@
 
 namespace rocket {
 namespace {
-
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-
-struct Pair { double a, b; };
-
-// Sums of two values over the block, in a fixed order; every thread gets them.
-__device__ __forceinline__ Pair block_sums(double a, double b) {
-    __shared__ double red[2][kWarps];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        a += __shfl_xor_sync(0xffffffffu, a, o);
-        b += __shfl_xor_sync(0xffffffffu, b, o);
-    }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) { red[0][threadIdx.x >> 5] = a; red[1][threadIdx.x >> 5] = b; }
-    __syncthreads();
-    a = b = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) { a += red[0][w]; b += red[1][w]; }
-    return {a, b};
-}
-
-template <class TX, class TY, class TW>
-__global__ void __launch_bounds__(kThreads)
-norm_backward_rows_kernel(const TY* __restrict__ dy, int64_t dy_stride, const TX* __restrict__ x, int64_t x_stride, int N,
-                          int P, const TW* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
-                          TX* __restrict__ dx, int64_t dx_stride) {
-    for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
-        const float m = mean[n], r = rstd[n];
-        double s = 0.0, q = 0.0;
-        for (int64_t i = threadIdx.x; i < P; i += kThreads) {
-            const float u = to_float(dy[n * dy_stride + i]) * (gamma ? to_float(gamma[i]) : 1.0f);
-            const float xh = (to_float(x[n * x_stride + i]) - m) * r;
-            s += (double)u;
-            q += (double)u * (double)xh;
-        }
-        const Pair t = block_sums(s, q);
-        const float c1 = (float)(t.a / (double)P), c2 = (float)(t.b / (double)P);
-        for (int64_t i = threadIdx.x; i < P; i += kThreads) {
-            const float u = to_float(dy[n * dy_stride + i]) * (gamma ? to_float(gamma[i]) : 1.0f);
-            const float xh = (to_float(x[n * x_stride + i]) - m) * r;
-            dx[n * dx_stride + i] = from_float<TX>(r * (u - c1 - xh * c2));
-        }
-    }
-}
-
-// A block owns 32 columns, its warps share the rows.
-template <class TX, class TY, class TW>
-__global__ void __launch_bounds__(kThreads)
-norm_weight_grads_kernel(const TY* __restrict__ dy, int64_t dy_stride, const TX* __restrict__ x, int64_t x_stride, int N,
-                         int P, const float* __restrict__ mean, const float* __restrict__ rstd, TW* __restrict__ dgamma,
-                         TW* __restrict__ dbeta) {
-    __shared__ double red[2][kWarps][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t p = (int64_t)blockIdx.x * 32 + lane;
-    double s = 0.0, q = 0.0;
-    if (p < P)
-        for (int64_t n = warp; n < N; n += kWarps) {
-            const float d = to_float(dy[n * dy_stride + p]);
-            const float xh = (to_float(x[n * x_stride + p]) - mean[n]) * rstd[n];
-            s += (double)d;
-            q += (double)d * (double)xh;
-        }
-    red[0][warp][lane] = s;
-    red[1][warp][lane] = q;
-    __syncthreads();
-    if (warp == 0 && p < P) {
-        s = q = 0.0;
-        for (int w = 0; w < kWarps; ++w) { s += red[0][w][lane]; q += red[1][w][lane]; }
-        if (dgamma) dgamma[p] = from_float<TW>((float)q);
-        if (dbeta) dbeta[p] = from_float<TW>((float)s);
-    }
-}
 
 // Rows [N][P] of `bytes` bytes a value, `stride` values apart.
 struct Rows {
@@ -153,7 +73,7 @@ extern "C" int rocket_layer_norm(const void* x_dev, int x_type, int64_t x_stride
 }
 
 extern "C" int64_t rocket_layer_norm_backward_workspace(int N, int P) {
-    return N < 0 || P < 1 ? ROCKET_EINVAL : 0;
+    return N < 0 || P < 1 ? ROCKET_EINVAL : norm::backward_workspace(N, P);
 }
 
 extern "C" int rocket_layer_norm_backward(const void* dy_dev, int y_type, int64_t dy_stride, const void* x_dev, int x_type,
@@ -168,7 +88,7 @@ extern "C" int rocket_layer_norm_backward(const void* dy_dev, int y_type, int64_
         return ROCKET_EINVAL;
     if (N > 0 && (!dy_dev || !x_dev || !mean_dev || !rstd_dev)) return ROCKET_EINVAL;
     if (!stride_ok(N, P, dy_stride, false) || !stride_ok(N, P, x_stride, false) || (dx_dev && !stride_ok(N, P, dx_stride, true))) return ROCKET_EINVAL;
-    const int64_t need = rocket_layer_norm_backward_workspace(N, P);
+    const int64_t need = dgamma_dev || dbeta_dev ? rocket_layer_norm_backward_workspace(N, P) : 0;
     if (workspace_bytes < need || (need > 0 && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15u)))) return ROCKET_EINVAL;
     const int xb = float_type_bytes(x_type), wb = float_type_bytes(w_type);
     const Rows none = {0, 1, 1, 1, 1};
@@ -186,22 +106,7 @@ extern "C" int rocket_layer_norm_backward(const void* dy_dev, int y_type, int64_
         for (int p = 0; p < o; ++p) if (overlap(out[o], out[p])) return ROCKET_EINVAL;
     }
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const unsigned blocks = (unsigned)std::min(N, 148 * 8);
-    with_float_type(x_type, [&](auto* tx) {
-        with_float_type(y_type, [&](auto* ty) {
-            with_float_type(w_type, [&](auto* tw) {
-                if (dx_dev && N > 0) {
-                    norm_backward_rows_kernel<<<blocks, kThreads, 0, stream>>>((decltype(ty))dy_dev, dy_stride, (decltype(tx))x_dev, x_stride, N, P,
-                                                                               (decltype(tw))gamma_dev, mean_dev, rstd_dev, (decltype(tx))dx_dev, dx_stride);
-                    count_launch();
-                }
-                if (dgamma_dev || dbeta_dev) {
-                    norm_weight_grads_kernel<<<(unsigned)(((int64_t)P + 31) / 32), kThreads, 0, stream>>>((decltype(ty))dy_dev, dy_stride, (decltype(tx))x_dev, x_stride, N, P,
-                                                                                                 mean_dev, rstd_dev, (decltype(tw))dgamma_dev, (decltype(tw))dbeta_dev);
-                    count_launch();
-                }
-            });
-        });
-    });
-    return status_of(cudaGetLastError());
+    const norm::Backward a = {dy_dev, x_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, dgamma_dev, dbeta_dev, static_cast<float*>(workspace_dev),
+                              dy_stride, x_stride, dx_stride, N, P, y_type, x_type, w_type};
+    return status_of(norm::launch_backward(a, stream));
 }

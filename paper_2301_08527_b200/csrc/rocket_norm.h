@@ -22,5 +22,23 @@ struct Forward {
 
 cudaError_t launch_forward(const Forward& a, cudaStream_t stream);
 
+struct Backward {
+    const void* dy;
+    const void* x;
+    const void* gamma;    // nullptr: ones
+    const float* mean;
+    const float* rstd;
+    void* dx;             // nullptr: not wanted, as dgamma and dbeta
+    void* dgamma;
+    void* dbeta;
+    float* partial;       // workspace
+    int64_t dy_stride, x_stride, dx_stride;
+    int N, P, y_type, x_type, w_type;
+};
+
+// Bytes of workspace for the gradients of gamma and beta.
+int64_t backward_workspace(int N, int P);
+cudaError_t launch_backward(const Backward& a, cudaStream_t stream);
+
 }  // namespace norm
 }  // namespace rocket

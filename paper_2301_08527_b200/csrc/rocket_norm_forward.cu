@@ -8,82 +8,16 @@
 // Who has a row: a warp where it is short, a block, or the blocks of a cluster where rows are few or longer than a block's
 // registers (each block sums its contiguous part, the sums meet in distributed shared memory).  The owners stay and go through
 // the rows in turn.
-#include <cooperative_groups.h>
-
 #include <algorithm>
 
 #include "rocket_float_types.cuh"
 #include "rocket_internal.h"
 #include "rocket_norm.h"
+#include "rocket_norm_sums.cuh"
 
 namespace rocket {
 namespace norm {
 namespace {
-
-namespace cg = cooperative_groups;
-
-constexpr int kMostParts = 8;
-
-enum Owner { kWarp, kBlock, kCluster };
-
-// Sums of a value over all threads that own the row, the same bits in each.  The two reductions of a row have buffers of their own,
-// so that one barrier each is enough: a warp that writes for the next row has passed the other's, behind everybody's reads.
-__device__ __forceinline__ float add_lanes(float v, int from) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (o <= from) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
-template <Owner OWNER>
-__device__ __forceinline__ float row_sum(float v, int parts, int rank, int half) {
-    v = add_lanes(v, 16);
-    if constexpr (OWNER != kWarp) {
-        __shared__ float red[32];
-        const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-        if (lane == 0) red[threadIdx.x >> 5] = v;
-        __syncthreads();
-        const int l = half ? lane & (2 * half - 1) : 0;                     // 2 half: the warps, rounded up to a power of two
-        v = add_lanes(l < warps ? red[l] : 0.0f, half);
-        if constexpr (OWNER == kCluster) {
-            __shared__ float share[kMostParts];
-            cg::cluster_group cluster = cg::this_cluster();
-            if ((int)threadIdx.x < parts) *cluster.map_shared_rank(&share[rank], threadIdx.x) = v;
-            cluster.sync();
-            v = share[0];
-            for (int p = 1; p < parts; ++p) v += share[p];
-        }
-    }
-    return v;
-}
-
-// The same of two values: each half of a warp goes on with one of them, which saves nearly half of the shuffles.
-template <Owner OWNER>
-__device__ __forceinline__ float2 row_sums(float2 v, int parts, int rank, int half) {
-    const int lane = threadIdx.x & 31;
-    const bool upper = lane >= 16;
-    float s = (upper ? v.y : v.x) + __shfl_xor_sync(0xffffffffu, upper ? v.x : v.y, 16);
-    s = add_lanes(s, 8);
-    if constexpr (OWNER != kWarp) {
-        __shared__ float red[2][32];
-        const int warps = blockDim.x >> 5;
-        if ((lane & 15) == 0) red[lane >> 4][threadIdx.x >> 5] = s;
-        __syncthreads();
-        const int l = lane & 15;
-        s = (l < warps ? red[lane >> 4][l] : 0.0f) + (l + 16 < warps ? red[lane >> 4][l + 16] : 0.0f);
-        s = add_lanes(s, 8);
-    }
-    v = make_float2(__shfl_sync(0xffffffffu, s, 0), __shfl_sync(0xffffffffu, s, 16));
-    if constexpr (OWNER == kCluster) {
-        __shared__ float2 share[kMostParts];
-        cg::cluster_group cluster = cg::this_cluster();
-        if ((int)threadIdx.x < parts) *cluster.map_shared_rank(&share[rank], threadIdx.x) = v;
-        cluster.sync();
-        v = share[0];
-        for (int p = 1; p < parts; ++p) { v.x += share[p].x; v.y += share[p].y; }
-    }
-    return v;
-}
 
 // W values per word, NV words per thread.  HOLD: a thread's values of gamma and beta stay in registers.
 template <class T, int W, int NV, Owner OWNER, bool HOLD>
@@ -159,7 +93,7 @@ rows_kernel(const Forward a, int parts, int half, float unit) {
                     s2.x += f[k][j];
                     s2.y = fmaf(f[k][j], f[k][j], s2.y);
                 }
-        s2 = row_sums<OWNER>(s2, parts, rank, half);
+        s2 = row_sums<OWNER>(s2, parts, rank, 0);
         const float rest = s2.x * over_p;
         const float v = fmaf(-rest, rest, s2.y * over_p), r = rsqrtf((v < 0.0f ? 0.0f : v) + a.eps);      // a NaN stays one
         const float off = -rest * r;
@@ -231,22 +165,12 @@ __global__ void __launch_bounds__(kLongThreads) long_rows_kernel(const Forward a
     }
 }
 
-constexpr int kSms = 148;
-
-int round32(int v) { return (v + 31) / 32 * 32; }
-
-// Sum's scale: the largest power of two that is at most 1 / P.  half: as row_sum takes it.
+// Sum's scale: the largest power of two that is at most 1 / P.
 float unit_of(int P) {
     int bits = 0;
     while ((int64_t(1) << bits) < P) ++bits;
     return ldexpf(1.0f, -bits);
 }
-int half_of(int threads) {
-    int half = 0;
-    while (std::max(2 * half, 1) < threads / 32) half = std::max(2 * half, 1);
-    return half;
-}
-
 template <class T, int W, int NV, Owner OWNER, bool HOLD>
 cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream) {
     auto kernel = rows_kernel<T, W, NV, OWNER, HOLD>;
@@ -269,15 +193,6 @@ cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream
     e = cudaLaunchKernelEx(&cfg, kernel, a, parts, half_of(threads), unit_of(a.P));
     count_launch();
     return e;
-}
-
-template <int N> using Int = std::integral_constant<int, N>;
-
-// Calls f with the constant `v` of LO .. HI.
-template <int LO, int HI, class F>
-cudaError_t with_int(int v, F&& f) {
-    if constexpr (LO < HI) if (v > LO) return with_int<LO + 1, HI>(v, f);
-    return f(Int<LO>());
 }
 
 template <class T, int W>
