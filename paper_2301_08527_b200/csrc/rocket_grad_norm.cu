@@ -5,7 +5,9 @@
 // Squares and sums are kept in double precision: fp32 gradients of 1e-20 and 1e20 both have squares outside fp32.  The sums'
 // order depends on the sizes alone.
 //
-// Bound: memory.
+// Bound: memory.  Two kernels: the first leaves a sum per block, every block of the second adds those up for itself and scales.  The second
+// goes through the tensors from the end, where the first has just been: what still lies in the L2 cache is not fetched again.  Tensors may
+// begin anywhere; each chunk is taken in words of 16 bytes between its first and its last such border.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -19,16 +21,18 @@ namespace rocket {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kBlocks = 148 * 8;         // most blocks, and partial sums, of one launch
-constexpr int kTensors = 112;            // of one launch: the table travels in its arguments
-constexpr int64_t kChunk = 16384;        // values of one tensor that a block takes at a time
+constexpr int kBlocks = 148 * 4;         // most blocks, and partial sums, of one launch
+constexpr int kFewTensors = 64;          // of one launch: the table travels in its arguments, of which a short one is there sooner
+constexpr int kTensors = 900;
+constexpr int kChunk = 16384;            // values of one tensor that a block takes at a time
 
+template <int N>
 struct Table {
-    const void* g[kTensors];
-    void* out[kTensors];
-    int64_t size[kTensors];
-    int first[kTensors + 1];             // chunk with which the tensor begins
-    uint8_t g_type[kTensors], out_type[kTensors];
+    const void* g[N];
+    void* out[N];
+    int64_t size[N];
+    int first[N + 1];                    // chunk with which the tensor begins
+    uint8_t g_type[N], out_type[N];
     int tensors;
 };
 
@@ -46,58 +50,114 @@ __device__ __forceinline__ double block_sum(double a) {
 }
 
 // The tensor that a chunk belongs to.
-__device__ __forceinline__ int tensor_of(const Table& t, int chunk) {
+template <int N>
+__device__ __forceinline__ int tensor_of(const Table<N>& t, int chunk) {
     int lo = 0, hi = t.tensors;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        (t.first[mid] <= chunk ? lo : hi) = mid;
+        if (t.first[mid] <= chunk) lo = mid;
+        else hi = mid;
     }
     return lo;
 }
 
-template <class T>
-__device__ __forceinline__ double sum_squares(const void* g, int64_t beg, int64_t end) {
-    double s = 0.0;
-    for (int64_t i = beg + threadIdx.x; i < end; i += kThreads) {
-        const double v = (double)to_float(static_cast<const T*>(g)[i]);
-        s += v * v;
+// Calls f(values, how many, position) for the words and single values of p[0 .. n) that fall to this thread, a few words at a time.
+template <class T, class F>
+__device__ __forceinline__ void for_chunk(const T* __restrict__ p, int n, F&& f) {
+    constexpr int W = 16 / (int)sizeof(T), U = 4;
+    const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
+    const int words = (n - head) / W, tail = head + words * W;
+    const T* __restrict__ body = p + head;
+    for (int i = threadIdx.x; i < words; i += U * kThreads) {
+        Packed<T, W> v[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (i + k * kThreads < words) v[k] = load_packed<T, W>(body + (i + k * kThreads) * W);
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (i + k * kThreads < words) {
+                float x[W];
+                unpack<T, W>(v[k], x);
+                f(x, head + (i + k * kThreads) * W);
+            }
     }
-    return s;
+    const int single = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - head;
+    if (single < n) {
+        const float x[1] = {to_float(p[single])};
+        f(x, single);
+    }
 }
 
-__global__ void __launch_bounds__(kThreads) squares_kernel(const __grid_constant__ Table t, double* __restrict__ part) {
-    double s = 0.0;
+template <class T>
+__device__ __forceinline__ void add_squares(const void* g, int64_t beg, int n, double (&s)[4]) {
+    for_chunk<T>(static_cast<const T*>(g) + beg, n, [&](const auto& x, int) {
+        constexpr int W = sizeof(x) / sizeof(float);
+#pragma unroll
+        for (int j = 0; j < W; ++j) s[j & 3] = fma((double)x[j], (double)x[j], s[j & 3]);
+    });
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads, 4) squares_kernel(const __grid_constant__ Table<N> t, double* __restrict__ part) {
+    double s[4] = {};
     for (int c = blockIdx.x; c < t.first[t.tensors]; c += gridDim.x) {
         const int k = tensor_of(t, c);
-        const int64_t beg = (int64_t)(c - t.first[k]) * kChunk, end = min(t.size[k], beg + kChunk);
-        s += t.g_type[k] == ROCKET_F32 ? sum_squares<float>(t.g[k], beg, end)
-             : t.g_type[k] == ROCKET_F16 ? sum_squares<__half>(t.g[k], beg, end) : sum_squares<__nv_bfloat16>(t.g[k], beg, end);
+        const int64_t beg = (int64_t)(c - t.first[k]) * kChunk;
+        const int n = (int)min((int64_t)kChunk, t.size[k] - beg);
+        if (t.g_type[k] == ROCKET_F32) add_squares<float>(t.g[k], beg, n, s);
+        else if (t.g_type[k] == ROCKET_F16) add_squares<__half>(t.g[k], beg, n, s);
+        else add_squares<__nv_bfloat16>(t.g[k], beg, n, s);
     }
-    s = block_sum(s);
-    if (threadIdx.x == 0) part[blockIdx.x] = s;
+    const double sum = block_sum((s[0] + s[1]) + (s[2] + s[3]));
+    if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-__global__ void __launch_bounds__(kThreads) norm_kernel(const double* __restrict__ part, int n, float* __restrict__ norm) {
+__device__ __forceinline__ float norm_of(const double* __restrict__ part, int n) {
     double s = 0.0;
     for (int i = threadIdx.x; i < n; i += kThreads) s += part[i];
-    s = block_sum(s);
-    if (threadIdx.x == 0) *norm = (float)sqrt(s);
+    return (float)sqrt(block_sum(s));
+}
+
+__global__ void __launch_bounds__(kThreads) norm_kernel(const double* __restrict__ part, int parts, float* __restrict__ norm) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const float n = norm_of(part, parts);
+    if (threadIdx.x == 0) *norm = n;
 }
 
 template <class TG, class TO>
-__device__ __forceinline__ void scale(const void* g, void* out, int64_t beg, int64_t end, float c) {
-    for (int64_t i = beg + threadIdx.x; i < end; i += kThreads)
-        static_cast<TO*>(out)[i] = from_float<TO>(to_float(static_cast<const TG*>(g)[i]) * c);
+__device__ __forceinline__ void scale(const void* g, void* out, int64_t beg, int n, float c) {
+    TO* __restrict__ to = static_cast<TO*>(out) + beg;
+    for_chunk<TG>(static_cast<const TG*>(g) + beg, n, [&](const auto& x, int at) {
+        constexpr int W = sizeof(x) / sizeof(float);
+        float o[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) o[j] = x[j] * c;
+        if (reinterpret_cast<uintptr_t>(to + at) % Packed<TO, W>::kWord == 0) {
+            store_packed<TO, W>(to + at, o);
+        } else {
+#pragma unroll
+            for (int j = 0; j < W; ++j) to[at + j] = from_float<TO>(o[j]);
+        }
+    });
 }
 
-__global__ void __launch_bounds__(kThreads) scale_kernel(const __grid_constant__ Table t, const float* __restrict__ norm, float max_norm) {
-    const float q = max_norm / (*norm + 1e-6f), c = q > 1.0f ? 1.0f : q;      // a NaN stays one
-    for (int i = blockIdx.x; i < t.first[t.tensors]; i += gridDim.x) {
-        const int k = tensor_of(t, i);
-        const int64_t beg = (int64_t)(i - t.first[k]) * kChunk, end = min(t.size[k], beg + kChunk);
-        if (t.g_type[k] == ROCKET_F32) scale<float, float>(t.g[k], t.out[k], beg, end, c);
-        else if (t.g_type[k] == ROCKET_F16) t.out_type[k] == ROCKET_F32 ? scale<__half, float>(t.g[k], t.out[k], beg, end, c) : scale<__half, __half>(t.g[k], t.out[k], beg, end, c);
-        else t.out_type[k] == ROCKET_F32 ? scale<__nv_bfloat16, float>(t.g[k], t.out[k], beg, end, c) : scale<__nv_bfloat16, __nv_bfloat16>(t.g[k], t.out[k], beg, end, c);
+// in_place: every output is its own gradient, and a gradient that is not clipped stays as it is.
+template <int N>
+__global__ void __launch_bounds__(kThreads, 4) scale_kernel(const __grid_constant__ Table<N> t, const double* __restrict__ part, int parts,
+                                                         float* __restrict__ norm, float max_norm, bool in_place) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const float n = norm_of(part, parts), q = max_norm / (n + 1e-6f), c = q > 1.0f ? 1.0f : q;      // a NaN stays one
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
+    if (in_place && c == 1.0f) return;
+    const int chunks = t.first[t.tensors];
+    for (int i = blockIdx.x; i < chunks; i += gridDim.x) {
+        const int chunk = chunks - 1 - i, k = tensor_of(t, chunk);
+        const int64_t beg = (int64_t)(chunk - t.first[k]) * kChunk;
+        const int len = (int)min((int64_t)kChunk, t.size[k] - beg);
+        const bool wide = t.out_type[k] == ROCKET_F32;
+        if (t.g_type[k] == ROCKET_F32) scale<float, float>(t.g[k], t.out[k], beg, len, c);
+        else if (t.g_type[k] == ROCKET_F16) wide ? scale<__half, float>(t.g[k], t.out[k], beg, len, c) : scale<__half, __half>(t.g[k], t.out[k], beg, len, c);
+        else wide ? scale<__nv_bfloat16, float>(t.g[k], t.out[k], beg, len, c) : scale<__nv_bfloat16, __nv_bfloat16>(t.g[k], t.out[k], beg, len, c);
     }
 }
 
@@ -109,14 +169,11 @@ int status_of(cudaError_t e) {
 
 using Span = std::pair<uintptr_t, uintptr_t>;
 
-// Whether two of the spans share a byte (sorts them).
-bool any_overlap(std::vector<Span>& s) {
-    std::sort(s.begin(), s.end());
-    for (size_t i = 1; i < s.size(); ++i) if (s[i].first < s[i - 1].second) return true;
-    return false;
+void sort_spans(std::vector<Span>& s) {
+    if (!std::is_sorted(s.begin(), s.end())) std::sort(s.begin(), s.end());
 }
 
-int64_t workspace_bytes_for(int count) { return 16 + (int64_t)sizeof(double) * kBlocks * ((count + (int64_t)kTensors - 1) / kTensors); }
+int64_t workspace_bytes_for(int count) { return (int64_t)sizeof(double) * kBlocks * std::max<int64_t>(1, (count + (int64_t)kTensors - 1) / kTensors); }
 
 // The arguments of both entry points; clip: whether gradients are written, to `out` or, where it is NULL, in place.
 int check(int count, const void* const* grads, const int64_t* sizes, const int32_t* types, bool clip, void* const* out, const int32_t* out_types,
@@ -125,7 +182,11 @@ int check(int count, const void* const* grads, const int64_t* sizes, const int32
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u) || workspace_bytes < workspace_bytes_for(count)) return ROCKET_EINVAL;
     if (count > 0 && (!grads || !sizes || !types || (out && !out_types))) return ROCKET_EINVAL;
     const Span own[] = {{(uintptr_t)norm, (uintptr_t)norm + 4}, {(uintptr_t)workspace, (uintptr_t)workspace + (uintptr_t)workspace_bytes_for(count)}};
-    std::vector<Span> written(own, own + 2), read;
+    auto meets = [](const Span& a, const Span& b) { return a.first < b.second && b.first < a.second; };
+    if (meets(own[0], own[1])) return ROCKET_EINVAL;
+    std::vector<Span> written, read;
+    if (clip) written.reserve((size_t)count);
+    if (out) read.reserve((size_t)count);
     int64_t chunks = 0;
     for (int i = 0; i < count; ++i) {
         if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40) || !is_float_type(types[i])) return ROCKET_EINVAL;
@@ -133,15 +194,20 @@ int check(int count, const void* const* grads, const int64_t* sizes, const int32
         if (sizes[i] == 0) continue;
         chunks += (sizes[i] + kChunk - 1) / kChunk;
         const uintptr_t g = (uintptr_t)grads[i], o = out ? (uintptr_t)out[i] : g;
-        const int gb = float_type_bytes(types[i]), ob = out ? float_type_bytes(out_types[i]) : gb;
-        if (!g || !o || g % gb || o % ob) return ROCKET_EINVAL;
-        if (clip) written.push_back({o, o + (uintptr_t)sizes[i] * ob});
-        if (!clip || o != g || ob != gb) read.push_back({g, g + (uintptr_t)sizes[i] * gb});
+        const unsigned gb = (unsigned)float_type_bytes(types[i]), ob = out ? (unsigned)float_type_bytes(out_types[i]) : gb;
+        if (!g || !o || (g & (gb - 1)) || (o & (ob - 1))) return ROCKET_EINVAL;
+        const Span from = {g, g + (uintptr_t)sizes[i] * gb}, to = {o, o + (uintptr_t)sizes[i] * ob};
+        if (meets(from, own[0]) || meets(from, own[1])) return ROCKET_EINVAL;
+        if (!clip) continue;
+        if (meets(to, own[0]) || meets(to, own[1])) return ROCKET_EINVAL;
+        written.push_back(to);
+        if (o != g || ob != gb) read.push_back(from);
     }
     if (chunks > 0x7fffffff) return ROCKET_EUNSUPPORTED;
     // what is written overlaps nothing; what is read may overlap itself (one tensor under two names counts twice)
-    if (any_overlap(written)) return ROCKET_EINVAL;
-    std::sort(read.begin(), read.end());
+    sort_spans(written);
+    for (size_t i = 1; i < written.size(); ++i) if (written[i].first < written[i - 1].second) return ROCKET_EINVAL;
+    sort_spans(read);
     size_t w = 0;
     for (const Span& r : read) {
         while (w < written.size() && written[w].second <= r.first) ++w;
@@ -150,43 +216,82 @@ int check(int count, const void* const* grads, const int64_t* sizes, const int32
     return ROCKET_OK;
 }
 
-void fill(Table& t, int beg, int end, const void* const* grads, const int64_t* sizes, const int32_t* types, void* const* out, const int32_t* out_types) {
-    t.tensors = end - beg;
+struct Call {
+    int count;
+    const void* const* grads;
+    const int64_t* sizes;
+    const int32_t* types;
+    void* const* out;                    // nullptr: in place
+    const int32_t* out_types;
+};
+
+template <int N>
+void fill(Table<N>& t, const Call& c, int beg, int end) {
+    t.tensors = 0;
     t.first[0] = 0;
     for (int i = beg; i < end; ++i) {
-        const int k = i - beg;
-        t.g[k] = grads[i];
-        t.out[k] = out ? out[i] : const_cast<void*>(grads[i]);
-        t.size[k] = sizes[i];
-        t.g_type[k] = (uint8_t)types[i];
-        t.out_type[k] = (uint8_t)(out ? out_types[i] : types[i]);
-        t.first[k + 1] = t.first[k] + (int)((sizes[i] + kChunk - 1) / kChunk);
+        if (c.sizes[i] == 0) continue;
+        const int k = t.tensors++;
+        t.g[k] = c.grads[i];
+        t.out[k] = c.out ? c.out[i] : const_cast<void*>(c.grads[i]);
+        t.size[k] = c.sizes[i];
+        t.g_type[k] = (uint8_t)c.types[i];
+        t.out_type[k] = (uint8_t)(c.out ? c.out_types[i] : c.types[i]);
+        t.first[k + 1] = t.first[k] + (int)((c.sizes[i] + kChunk - 1) / kChunk);
     }
 }
 
-int run(int count, const void* const* grads, const int64_t* sizes, const int32_t* types, bool clip, void* const* out, const int32_t* out_types,
-        float max_norm, float* norm, void* workspace, cudaStream_t stream) {
-    double* part = static_cast<double*>(workspace);
+// A kernel that begins before its predecessor has ended, and waits for it by griddepcontrol.wait.
+template <class... A, class... B>
+cudaError_t launch_behind(void (*kernel)(A...), int blocks, cudaStream_t stream, B&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    count_launch();
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<B>(args)...);
+}
+
+template <int N>
+cudaError_t run(const Call& c, bool clip, float max_norm, float* norm, double* part, cudaStream_t stream) {
+    Table<N> t;
     int parts = 0;
-    Table t;
-    for (int beg = 0; beg < count; beg += kTensors) {
-        fill(t, beg, std::min(count, beg + kTensors), grads, sizes, types, out, out_types);
+    for (int beg = 0; beg < c.count; beg += N) {
+        fill(t, c, beg, std::min(c.count, beg + N));
         const int blocks = std::min(t.first[t.tensors], kBlocks);
         if (!blocks) continue;
-        squares_kernel<<<blocks, kThreads, 0, stream>>>(t, part + parts);
+        squares_kernel<N><<<blocks, kThreads, 0, stream>>>(t, part + parts);
         count_launch();
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
         parts += blocks;
     }
-    norm_kernel<<<1, kThreads, 0, stream>>>(part, parts, norm);
-    count_launch();
-    for (int beg = 0; clip && beg < count; beg += kTensors) {
-        fill(t, beg, std::min(count, beg + kTensors), grads, sizes, types, out, out_types);
+    if (!clip || parts == 0) return launch_behind(norm_kernel, 1, stream, (const double*)part, parts, norm);
+    for (int beg = (c.count - 1) / N * N; beg >= 0; beg -= N) {
+        if (c.count > N) fill(t, c, beg, std::min(c.count, beg + N));
         const int blocks = std::min(t.first[t.tensors], kBlocks);
         if (!blocks) continue;
-        scale_kernel<<<blocks, kThreads, 0, stream>>>(t, norm, max_norm);
-        count_launch();
+        const cudaError_t e = launch_behind(scale_kernel<N>, blocks, stream, t, (const double*)part, parts, norm, max_norm, c.out == nullptr);
+        if (e != cudaSuccess) return e;
     }
-    return status_of(cudaGetLastError());
+    return cudaSuccess;
+}
+
+int call(const Call& c, bool clip, float max_norm, float* norm, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+    try {
+        const int st = check(c.count, c.grads, c.sizes, c.types, clip, c.out, c.out_types, norm, workspace, workspace_bytes);
+        if (st != ROCKET_OK) return st;
+    } catch (const std::bad_alloc&) {
+        return ROCKET_ENOMEM;
+    }
+    auto* part = static_cast<double*>(workspace);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    return status_of(c.count <= kFewTensors ? run<kFewTensors>(c, clip, max_norm, norm, part, stream) : run<kTensors>(c, clip, max_norm, norm, part, stream));
 }
 
 }  // namespace
@@ -198,24 +303,12 @@ extern "C" int64_t rocket_grad_norm_workspace(int count) { return count < 0 ? RO
 
 extern "C" int rocket_grad_norm(int count, const void* const* grads_dev, const int64_t* sizes, const int32_t* types, float* norm_dev,
                                 void* workspace_dev, int64_t workspace_bytes, void* cuda_stream) {
-    try {
-        const int st = check(count, grads_dev, sizes, types, false, nullptr, nullptr, norm_dev, workspace_dev, workspace_bytes);
-        if (st != ROCKET_OK) return st;
-    } catch (const std::bad_alloc&) {
-        return ROCKET_ENOMEM;
-    }
-    return run(count, grads_dev, sizes, types, false, nullptr, nullptr, 0.0f, norm_dev, workspace_dev, static_cast<cudaStream_t>(cuda_stream));
+    return call({count, grads_dev, sizes, types, nullptr, nullptr}, false, 0.0f, norm_dev, workspace_dev, workspace_bytes, cuda_stream);
 }
 
 extern "C" int rocket_clip_grad_norm(int count, const void* const* grads_dev, const int64_t* sizes, const int32_t* types,
                                      void* const* out_dev, const int32_t* out_types, float max_norm, float* norm_dev,
                                      void* workspace_dev, int64_t workspace_bytes, void* cuda_stream) {
     if (!(max_norm >= 0.0f)) return ROCKET_EINVAL;
-    try {
-        const int st = check(count, grads_dev, sizes, types, true, out_dev, out_types, norm_dev, workspace_dev, workspace_bytes);
-        if (st != ROCKET_OK) return st;
-    } catch (const std::bad_alloc&) {
-        return ROCKET_ENOMEM;
-    }
-    return run(count, grads_dev, sizes, types, true, out_dev, out_types, max_norm, norm_dev, workspace_dev, static_cast<cudaStream_t>(cuda_stream));
+    return call({count, grads_dev, sizes, types, out_dev, out_types}, true, max_norm, norm_dev, workspace_dev, workspace_bytes, cuda_stream);
 }
