@@ -3,6 +3,7 @@
 torch is used for device memory and streams; tensors are passed to the library as raw device
 pointers together with the current CUDA stream.
 """
+import array
 import ctypes
 import os
 
@@ -255,19 +256,22 @@ class RocketParams:
 
 _torch = None
 _current_stream = None
+_current_device = None
 
 
 def _t():
     """torch, imported at the first call that needs it (importing this module does not)."""
-    global _torch, _current_stream
+    global _torch, _current_stream, _current_device
     if _torch is None:
         import torch
         # the raw handle of the current stream, without building a Stream object (1.5 us) on every call
         raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
         if raw is not None and device is not None:
             _current_stream = lambda: raw(device())  # noqa: E731
+            _current_device = device
         else:
             _current_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+            _current_device = torch.cuda.current_device
         _torch = torch
     return _torch
 
@@ -436,12 +440,12 @@ def _types():
 
 def _on_device(call, device, where):
     """Runs call(stream) with `device` current, on that device's current stream."""
-    torch = _t()
-    if device.index == torch.cuda.current_device():
-        _check(call(_stream()), where)
+    index = device.index
+    if index == _current_device():
+        _check(call(_current_stream()), where)
     else:
-        with torch.cuda.device(device):
-            _check(call(_stream()), where)
+        with _torch.cuda.device(index):
+            _check(call(_current_stream()), where)
 
 
 def _rows(t, name, shape=None, device=None, dtype=None):
@@ -501,23 +505,28 @@ def rocket_layer_norm(feat, gamma=None, beta=None, eps=1e-5, out=None, out_dtype
     type, or None.  Returns (out, mean, rstd), the statistics fp32, one per row, or None without want_stats."""
     torch = _t()
     x, xt, xs, N, P = _rows(feat, "feat")
-    device = feat.device
-    y = out if out is not None else torch.empty(feat.shape, dtype=out_dtype or feat.dtype, device=device)
-    yp, yt, ys, _, _ = _rows(y, "out", feat.shape, device, out_dtype)
+    device, shape = feat.device, feat.shape
+    y = out
+    if y is not None:
+        yp, yt, ys, _, _ = _rows(y, "out", shape, device, out_dtype)
+    else:
+        y = feat.new_empty(shape) if out_dtype is None else feat.new_empty(shape, dtype=out_dtype)
+        yp, yt, ys = y.data_ptr(), _types().get(y.dtype), P
+        if yt is None:
+            raise TypeError("out_dtype must be float32, float16 or bfloat16")
     g, wt = _vector(gamma, P, "gamma", device)
     b, bt = _vector(beta, P, "beta", device)
-    if wt is not None and bt is not None and wt != bt:
+    if wt is None:
+        wt = bt if bt is not None else 0
+    elif bt is not None and wt != bt:
         raise TypeError("gamma and beta must be of one dtype")
-    wt = wt if wt is not None else bt if bt is not None else 0
     mean, rstd = mean_out, rstd_out
-    if want_stats:
-        lead = feat.shape[:-1]
-        if mean is None:
-            mean = torch.empty(lead, dtype=torch.float32, device=device)
-        if rstd is None:
-            rstd = torch.empty(lead, dtype=torch.float32, device=device)
-    mp, _ = _vector(mean, N, "mean_out", device, torch.float32)
-    rp, _ = _vector(rstd, N, "rstd_out", device, torch.float32)
+    if want_stats and mean is None:
+        mean = feat.new_empty(shape[:-1], dtype=torch.float32)
+    if want_stats and rstd is None:
+        rstd = torch.empty_like(mean)
+    mp = _vector(mean, N, "mean_out", device, torch.float32)[0]
+    rp = _vector(rstd, N, "rstd_out", device, torch.float32)[0]
     fn = (_lib or load_library()).rocket_layer_norm
     _on_device(lambda s: fn(x, xt, xs, N, P, g, b, wt, eps, yp, yt, ys, mp, rp, s), device, "rocket_layer_norm")
     return y, mean, rstd
@@ -529,10 +538,10 @@ def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dg
     Returns (dx of feat's type, dgamma, dbeta of gamma's type or weight_dtype); what is not wanted is None."""
     torch = _t()
     x, xt, xs, N, P = _rows(feat, "feat")
-    device = feat.device
-    d, yt, ds, _, _ = _rows(dy, "dy", feat.shape, device)
-    mp, _ = _vector(mean, N, "mean", device, torch.float32)
-    rp, _ = _vector(rstd, N, "rstd", device, torch.float32)
+    device, shape = feat.device, feat.shape
+    d, yt, ds, _, _ = _rows(dy, "dy", shape, device)
+    mp = _vector(mean, N, "mean", device, torch.float32)[0]
+    rp = _vector(rstd, N, "rstd", device, torch.float32)[0]
     if mp is None or rp is None:
         raise TypeError("mean and rstd must be the statistics of the forward pass")
     g, wt = _vector(gamma, P, "gamma", device)
@@ -541,26 +550,29 @@ def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dg
             dbeta_out.dtype if dbeta_out is not None else torch.float32
     elif gamma is not None and gamma.dtype is not weight_dtype:
         raise TypeError("weight_dtype must be gamma's")
+    if wt is None:
+        wt = _types().get(weight_dtype)
+        if wt is None:
+            raise TypeError("weight_dtype must be float32, float16 or bfloat16")
     dx, dg, db = dx_out, dgamma_out, dbeta_out
-    if dx is None and want_dx:
-        dx = torch.empty(feat.shape, dtype=feat.dtype, device=device)
-    if want_weights:
-        if dg is None:
-            dg = torch.empty((P,), dtype=weight_dtype, device=device)
-        if db is None:
-            db = torch.empty((P,), dtype=weight_dtype, device=device)
     dxp, dxs = None, 0
     if dx is not None:
-        dxp, _, dxs, _, _ = _rows(dx, "dx_out", feat.shape, device, feat.dtype)
-    dgp, wt1 = _vector(dg, P, "dgamma_out", device, weight_dtype)
-    dbp, wt2 = _vector(db, P, "dbeta_out", device, weight_dtype)
-    wt = wt if wt is not None else wt1 if wt1 is not None else wt2 if wt2 is not None else 0
+        dxp, _, dxs, _, _ = _rows(dx, "dx_out", shape, device, feat.dtype)
+    elif want_dx:
+        dx = feat.new_empty(shape)
+        dxp, dxs = dx.data_ptr(), P
+    if want_weights and dg is None:
+        dg = feat.new_empty((P,), dtype=weight_dtype) if gamma is None else torch.empty_like(gamma)
+    if want_weights and db is None:
+        db = torch.empty_like(dg)
+    dgp = _vector(dg, P, "dgamma_out", device, weight_dtype)[0]
+    dbp = _vector(db, P, "dbeta_out", device, weight_dtype)[0]
     lib = _lib or load_library()
-    need = lib.rocket_layer_norm_backward_workspace(N, P) if dg is not None or db is not None else 0
-    ws = torch.empty((need,), dtype=torch.uint8, device=device) if need > 0 else None
-    wp = ws.data_ptr() if need > 0 else None
+    need = max(lib.rocket_layer_norm_backward_workspace(N, P), 0) if dg is not None or db is not None else 0
+    ws = mean.new_empty(need // 4) if need else None
+    wp = ws.data_ptr() if need else None
     fn = lib.rocket_layer_norm_backward
-    _on_device(lambda s: fn(d, yt, ds, x, xt, xs, N, P, g, wt, mp, rp, dxp, dxs, dgp, dbp, wp, max(need, 0), s), device,
+    _on_device(lambda s: fn(d, yt, ds, x, xt, xs, N, P, g, wt, mp, rp, dxp, dxs, dgp, dbp, wp, need, s), device,
                "rocket_layer_norm_backward")
     return dx, dg, db
 
@@ -579,66 +591,72 @@ def _dense(t):
 
 
 def _tensor_list(ts, name):
-    """(addresses, sizes, type codes) as arrays, and the device, of a sequence of CUDA tensors."""
+    """(count, addresses, sizes, type codes, device, all contiguous) of a sequence of CUDA tensors, as arrays.  Long lists are the
+    rule, so every property is asked for in one sweep."""
+    Tensor = _t().Tensor
     types = _types()
-    n = len(ts)
-    ptrs, sizes, codes = (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
-    device = None
-    for i, t in enumerate(ts):
-        try:
-            code = types.get(t.dtype)
-            if code is None or not t.is_cuda or not _dense(t):
-                raise TypeError("%s must be dense CUDA tensors of float32, float16 or bfloat16" % name)
-        except AttributeError:
-            raise TypeError("%s must be a sequence of tensors" % name) from None
-        if device is None:
-            device = t.device
-        elif t.device != device:
-            raise ValueError("%s must be on one device" % name)
-        ptrs[i], sizes[i], codes[i] = t.data_ptr(), t.numel(), code
-    return ptrs, sizes, codes, device
+    if not isinstance(ts, (list, tuple)):
+        raise TypeError("%s must be a list or tuple of tensors" % name)
+    if not ts:
+        return 0, None, None, None, None, True
+    try:
+        kinds = [t.dtype for t in ts]
+        codes = [types[k] for k in kinds]
+        devices = set(map(Tensor.get_device, ts))
+        contiguous = all(map(Tensor.is_contiguous, ts))
+        if -1 in devices or not ts[0].is_cuda or not (contiguous or all(map(_dense, ts))):
+            raise KeyError
+        ptrs, sizes = array.array("q", map(Tensor.data_ptr, ts)), array.array("q", map(Tensor.numel, ts))
+    except (KeyError, AttributeError, TypeError):
+        raise TypeError("%s must be dense CUDA tensors of float32, float16 or bfloat16" % name) from None
+    if len(devices) != 1:
+        raise ValueError("%s must be on one device" % name)
+    return len(ts), ptrs, sizes, array.array("i", codes), ts[0].device, contiguous
 
 
-def _norm_buffers(lib, count, device, norm_out):
+def _address(a):
+    return None if a is None else a.buffer_info()[0]
+
+
+def _norm_buffers(lib, count, grads, norm_out):
     torch = _t()
-    if device is None:
-        device = norm_out.device if norm_out is not None else torch.device("cuda", torch.cuda.current_device())
+    norm = norm_out
+    if norm is None:
+        norm = grads[0].new_empty(1, dtype=torch.float32) if count else torch.empty(1, dtype=torch.float32, device="cuda")
+    np_ = _vector(norm, 1, "norm_out", grads[0].device if count else norm.device, torch.float32)[0]
     need = lib.rocket_grad_norm_workspace(count)
-    ws = torch.empty((need,), dtype=torch.uint8, device=device)
-    norm = norm_out if norm_out is not None else torch.empty((1,), dtype=torch.float32, device=device)
-    return device, ws, need, norm, _vector(norm, 1, "norm_out", device, torch.float32)[0]
+    ws = norm.new_empty(need // 4)
+    return ws, ws.data_ptr(), need, norm, np_
 
 
 def rocket_grad_norm(grads, norm_out=None):
-    """2-norm of a gradient held in many tensors (a sequence of dense CUDA tensors of float32, float16 or bfloat16 on one
+    """2-norm of a gradient held in many tensors (a list or tuple of dense CUDA tensors of float32, float16 or bfloat16 on one
     device).  Returns it as a [1] float32 tensor."""
     lib = _lib or load_library()
-    ptrs, sizes, codes, device = _tensor_list(grads, "grads")
-    n = len(ptrs)
-    device, ws, need, norm, np_ = _norm_buffers(lib, n, device, norm_out)
-    wp = ws.data_ptr()
-    _on_device(lambda s: lib.rocket_grad_norm(n, ptrs, sizes, codes, np_, wp, need, s), device, "rocket_grad_norm")
+    n, ptrs, sizes, codes, _, _ = _tensor_list(grads, "grads")
+    ws, wp, need, norm, np_ = _norm_buffers(lib, n, grads, norm_out)
+    p, z, c = _address(ptrs), _address(sizes), _address(codes)
+    _on_device(lambda s: lib.rocket_grad_norm(n, p, z, c, np_, wp, need, s), norm.device, "rocket_grad_norm")
     return norm
 
 
 def rocket_clip_grad_norm(grads, max_norm, out=None, norm_out=None):
-    """Scales the gradient by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of out (each of its gradient's
-    shape and order of values, of its type or float32).  Returns (norm before clipping as a [1] float32 tensor, the clipped
+    """Scales the gradient by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of out (each with its gradient's
+    values in the same order, of its type or float32).  Returns (norm before clipping as a [1] float32 tensor, the clipped
     tensors)."""
     lib = _lib or load_library()
-    ptrs, sizes, codes, device = _tensor_list(grads, "grads")
-    n = len(ptrs)
-    op = oc = None
+    n, ptrs, sizes, codes, device, contiguous = _tensor_list(grads, "grads")
+    outs = out_codes = None
     if out is not None:
-        op, osizes, oc, odevice = _tensor_list(out, "out")
-        if len(out) != n or odevice != device:
-            raise ValueError("out must hold one tensor per gradient, on the same device")
-        for a, b in zip(grads, out):
-            if a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())):
-                raise ValueError("out must have the shapes and strides of the gradients")
-    device, ws, need, norm, np_ = _norm_buffers(lib, n, device, norm_out)
-    wp = ws.data_ptr()
-    _on_device(lambda s: lib.rocket_clip_grad_norm(n, ptrs, sizes, codes, op, oc, max_norm, np_, wp, need, s), device,
+        m, outs, out_sizes, out_codes, out_device, out_contiguous = _tensor_list(out, "out")
+        if m != n or out_sizes != sizes or out_device != device:
+            raise ValueError("out must hold one tensor per gradient, of its size, on the same device")
+        if not (contiguous and out_contiguous) and any(
+                a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
+            raise ValueError("out must have the shapes and strides of the gradients")
+    ws, wp, need, norm, np_ = _norm_buffers(lib, n, grads, norm_out)
+    p, z, c, o, oc = _address(ptrs), _address(sizes), _address(codes), _address(outs), _address(out_codes)
+    _on_device(lambda s: lib.rocket_clip_grad_norm(n, p, z, c, o, oc, max_norm, np_, wp, need, s), norm.device,
                "rocket_clip_grad_norm")
     return norm, grads if out is None else out
 

@@ -8,6 +8,8 @@
 // Bound: memory.  Two kernels: the first leaves a sum per block, every block of the second adds those up for itself and scales.  The second
 // goes through the tensors from the end, where the first has just been: what still lies in the L2 cache is not fetched again.  Tensors may
 // begin anywhere; each chunk is taken in words of 16 bytes between its first and its last such border.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -20,11 +22,17 @@
 namespace rocket {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 256;
 constexpr int kBlocks = 148 * 4;         // most blocks, and partial sums, of one launch
 constexpr int kFewTensors = 64;          // of one launch: the table travels in its arguments, of which a short one is there sooner
 constexpr int kTensors = 900;
-constexpr int kChunk = 16384;            // values of one tensor that a block takes at a time
+// Values of one tensor that a block takes at a time: few enough that a small gradient reaches every block, and at most so many that
+// finding a chunk's tensor costs nothing beside the chunk.
+constexpr int kLeastChunk = 1024, kMostChunk = 16384;
+constexpr int kSmall = 128 * 1024;       // values that one cluster deals with in one launch
+constexpr int kSmallBlocks = 8, kSmallThreads = 512;
 
 template <int N>
 struct Table {
@@ -33,10 +41,12 @@ struct Table {
     int64_t size[N];
     int first[N + 1];                    // chunk with which the tensor begins
     uint8_t g_type[N], out_type[N];
-    int tensors;
+    int tensors, chunk;
 };
 
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double a) {
+    constexpr int kWarps = THREADS / 32;
     __shared__ double red[kWarps];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
@@ -62,23 +72,23 @@ __device__ __forceinline__ int tensor_of(const Table<N>& t, int chunk) {
 }
 
 // Calls f(values, how many, position) for the words and single values of p[0 .. n) that fall to this thread, a few words at a time.
-template <class T, class F>
-__device__ __forceinline__ void for_chunk(const T* __restrict__ p, int n, F&& f) {
+template <int THREADS, class T, class F>
+__device__ __forceinline__ void for_chunk(const T* p, int n, F&& f) {
     constexpr int W = 16 / (int)sizeof(T), U = 4;
     const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
     const int words = (n - head) / W, tail = head + words * W;
-    const T* __restrict__ body = p + head;
-    for (int i = threadIdx.x; i < words; i += U * kThreads) {
+    const T* body = p + head;
+    for (int i = threadIdx.x; i < words; i += U * THREADS) {
         Packed<T, W> v[U];
 #pragma unroll
         for (int k = 0; k < U; ++k)
-            if (i + k * kThreads < words) v[k] = load_packed<T, W>(body + (i + k * kThreads) * W);
+            if (i + k * THREADS < words) v[k] = load_packed<T, W>(body + (i + k * THREADS) * W);
 #pragma unroll
         for (int k = 0; k < U; ++k)
-            if (i + k * kThreads < words) {
+            if (i + k * THREADS < words) {
                 float x[W];
                 unpack<T, W>(v[k], x);
-                f(x, head + (i + k * kThreads) * W);
+                f(x, head + (i + k * THREADS) * W);
             }
     }
     const int single = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - head;
@@ -88,46 +98,39 @@ __device__ __forceinline__ void for_chunk(const T* __restrict__ p, int n, F&& f)
     }
 }
 
-template <class T>
+template <int THREADS, class T>
 __device__ __forceinline__ void add_squares(const void* g, int64_t beg, int n, double (&s)[4]) {
-    for_chunk<T>(static_cast<const T*>(g) + beg, n, [&](const auto& x, int) {
+    for_chunk<THREADS, T>(static_cast<const T*>(g) + beg, n, [&](const auto& x, int) {
         constexpr int W = sizeof(x) / sizeof(float);
 #pragma unroll
         for (int j = 0; j < W; ++j) s[j & 3] = fma((double)x[j], (double)x[j], s[j & 3]);
     });
 }
 
-template <int N>
-__global__ void __launch_bounds__(kThreads, 4) squares_kernel(const __grid_constant__ Table<N> t, double* __restrict__ part) {
+// The block's sum of squares of every blocks-th chunk.
+template <int THREADS, int N>
+__device__ __forceinline__ double squares(const Table<N>& t, int block, int blocks) {
     double s[4] = {};
-    for (int c = blockIdx.x; c < t.first[t.tensors]; c += gridDim.x) {
+    for (int c = block; c < t.first[t.tensors]; c += blocks) {
         const int k = tensor_of(t, c);
-        const int64_t beg = (int64_t)(c - t.first[k]) * kChunk;
-        const int n = (int)min((int64_t)kChunk, t.size[k] - beg);
-        if (t.g_type[k] == ROCKET_F32) add_squares<float>(t.g[k], beg, n, s);
-        else if (t.g_type[k] == ROCKET_F16) add_squares<__half>(t.g[k], beg, n, s);
-        else add_squares<__nv_bfloat16>(t.g[k], beg, n, s);
+        const int64_t beg = (int64_t)(c - t.first[k]) * t.chunk;
+        const int n = (int)min((int64_t)t.chunk, t.size[k] - beg);
+        if (t.g_type[k] == ROCKET_F32) add_squares<THREADS, float>(t.g[k], beg, n, s);
+        else if (t.g_type[k] == ROCKET_F16) add_squares<THREADS, __half>(t.g[k], beg, n, s);
+        else add_squares<THREADS, __nv_bfloat16>(t.g[k], beg, n, s);
     }
-    const double sum = block_sum((s[0] + s[1]) + (s[2] + s[3]));
-    if (threadIdx.x == 0) part[blockIdx.x] = sum;
+    return block_sum<THREADS>((s[0] + s[1]) + (s[2] + s[3]));
 }
 
-__device__ __forceinline__ float norm_of(const double* __restrict__ part, int n) {
-    double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += kThreads) s += part[i];
-    return (float)sqrt(block_sum(s));
+__device__ __forceinline__ float factor(float norm, float max_norm) {
+    const float q = max_norm / (norm + 1e-6f);
+    return q > 1.0f ? 1.0f : q;          // a NaN stays one
 }
 
-__global__ void __launch_bounds__(kThreads) norm_kernel(const double* __restrict__ part, int parts, float* __restrict__ norm) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const float n = norm_of(part, parts);
-    if (threadIdx.x == 0) *norm = n;
-}
-
-template <class TG, class TO>
-__device__ __forceinline__ void scale(const void* g, void* out, int64_t beg, int n, float c) {
-    TO* __restrict__ to = static_cast<TO*>(out) + beg;
-    for_chunk<TG>(static_cast<const TG*>(g) + beg, n, [&](const auto& x, int at) {
+template <int THREADS, class TG, class TO>
+__device__ __forceinline__ void scale_chunk(const void* g, void* out, int64_t beg, int n, float c) {
+    TO* to = static_cast<TO*>(out) + beg;
+    for_chunk<THREADS, TG>(static_cast<const TG*>(g) + beg, n, [&](const auto& x, int at) {
         constexpr int W = sizeof(x) / sizeof(float);
         float o[W];
 #pragma unroll
@@ -141,24 +144,66 @@ __device__ __forceinline__ void scale(const void* g, void* out, int64_t beg, int
     });
 }
 
+template <int THREADS, int N>
+__device__ __forceinline__ void scale(const Table<N>& t, int block, int blocks, float c) {
+    const int chunks = t.first[t.tensors];
+    for (int i = block; i < chunks; i += blocks) {
+        const int at = chunks - 1 - i, k = tensor_of(t, at);
+        const int64_t beg = (int64_t)(at - t.first[k]) * t.chunk;
+        const int n = (int)min((int64_t)t.chunk, t.size[k] - beg);
+        const bool wide = t.out_type[k] == ROCKET_F32;
+        if (t.g_type[k] == ROCKET_F32) scale_chunk<THREADS, float, float>(t.g[k], t.out[k], beg, n, c);
+        else if (t.g_type[k] == ROCKET_F16) wide ? scale_chunk<THREADS, __half, float>(t.g[k], t.out[k], beg, n, c) : scale_chunk<THREADS, __half, __half>(t.g[k], t.out[k], beg, n, c);
+        else wide ? scale_chunk<THREADS, __nv_bfloat16, float>(t.g[k], t.out[k], beg, n, c) : scale_chunk<THREADS, __nv_bfloat16, __nv_bfloat16>(t.g[k], t.out[k], beg, n, c);
+    }
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads, 4) squares_kernel(const __grid_constant__ Table<N> t, double* __restrict__ part) {
+    const double sum = squares<kThreads>(t, blockIdx.x, gridDim.x);
+    if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+__device__ __forceinline__ float norm_of(const double* __restrict__ part, int n) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n; i += kThreads) s += part[i];
+    return (float)sqrt(block_sum<kThreads>(s));
+}
+
+__global__ void __launch_bounds__(kThreads) norm_kernel(const double* __restrict__ part, int parts, float* __restrict__ norm) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const float n = norm_of(part, parts);
+    if (threadIdx.x == 0) *norm = n;
+}
+
 // in_place: every output is its own gradient, and a gradient that is not clipped stays as it is.
 template <int N>
 __global__ void __launch_bounds__(kThreads, 4) scale_kernel(const __grid_constant__ Table<N> t, const double* __restrict__ part, int parts,
-                                                         float* __restrict__ norm, float max_norm, bool in_place) {
+                                                            float* __restrict__ norm, float max_norm, bool in_place) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const float n = norm_of(part, parts), q = max_norm / (n + 1e-6f), c = q > 1.0f ? 1.0f : q;      // a NaN stays one
+    const float n = norm_of(part, parts), c = factor(n, max_norm);
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
-    if (in_place && c == 1.0f) return;
-    const int chunks = t.first[t.tensors];
-    for (int i = blockIdx.x; i < chunks; i += gridDim.x) {
-        const int chunk = chunks - 1 - i, k = tensor_of(t, chunk);
-        const int64_t beg = (int64_t)(chunk - t.first[k]) * kChunk;
-        const int len = (int)min((int64_t)kChunk, t.size[k] - beg);
-        const bool wide = t.out_type[k] == ROCKET_F32;
-        if (t.g_type[k] == ROCKET_F32) scale<float, float>(t.g[k], t.out[k], beg, len, c);
-        else if (t.g_type[k] == ROCKET_F16) wide ? scale<__half, float>(t.g[k], t.out[k], beg, len, c) : scale<__half, __half>(t.g[k], t.out[k], beg, len, c);
-        else wide ? scale<__nv_bfloat16, float>(t.g[k], t.out[k], beg, len, c) : scale<__nv_bfloat16, __nv_bfloat16>(t.g[k], t.out[k], beg, len, c);
-    }
+    if (!(in_place && c == 1.0f)) scale<kThreads>(t, blockIdx.x, gridDim.x, c);
+}
+
+// Both in one launch for a small gradient, by the blocks of one cluster, whose sums meet in distributed shared memory; nothing is
+// written before the barrier behind which all of them have read everything.
+__global__ void __launch_bounds__(kSmallThreads) small_kernel(const __grid_constant__ Table<kFewTensors> t, float* __restrict__ norm, float max_norm, bool clip,
+                                                              bool in_place) {
+    __shared__ double share[kSmallBlocks];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");       // nobody writes to a block that does not run yet
+    const double sum = squares<kSmallThreads>(t, rank, kSmallBlocks);
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (threadIdx.x < kSmallBlocks) *cluster.map_shared_rank(&share[rank], threadIdx.x) = sum;
+    cluster.sync();
+    double s = share[0];
+#pragma unroll
+    for (int i = 1; i < kSmallBlocks; ++i) s += share[i];
+    const float n = (float)sqrt(s), c = factor(n, max_norm);
+    if (rank == 0 && threadIdx.x == 0) *norm = n;
+    if (clip && !(in_place && c == 1.0f)) scale<kSmallThreads>(t, rank, kSmallBlocks, c);
 }
 
 int status_of(cudaError_t e) {
@@ -192,7 +237,7 @@ int check(int count, const void* const* grads, const int64_t* sizes, const int32
         if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40) || !is_float_type(types[i])) return ROCKET_EINVAL;
         if (out && (!is_float_type(out_types[i]) || (out_types[i] != types[i] && out_types[i] != ROCKET_F32))) return ROCKET_EINVAL;
         if (sizes[i] == 0) continue;
-        chunks += (sizes[i] + kChunk - 1) / kChunk;
+        chunks += (sizes[i] + kMostChunk - 1) / kMostChunk;
         const uintptr_t g = (uintptr_t)grads[i], o = out ? (uintptr_t)out[i] : g;
         const unsigned gb = (unsigned)float_type_bytes(types[i]), ob = out ? (unsigned)float_type_bytes(out_types[i]) : gb;
         if (!g || !o || (g & (gb - 1)) || (o & (ob - 1))) return ROCKET_EINVAL;
@@ -225,9 +270,17 @@ struct Call {
     const int32_t* out_types;
 };
 
+// A power of two, the largest that gives every block of a launch a chunk.
+int chunk_of(int64_t total) {
+    int chunk = kMostChunk;
+    while (chunk > kLeastChunk && total < (int64_t)kBlocks * chunk) chunk /= 2;
+    return chunk;
+}
+
 template <int N>
-void fill(Table<N>& t, const Call& c, int beg, int end) {
+void fill(Table<N>& t, const Call& c, int beg, int end, int chunk) {
     t.tensors = 0;
+    t.chunk = chunk;
     t.first[0] = 0;
     for (int i = beg; i < end; ++i) {
         if (c.sizes[i] == 0) continue;
@@ -237,7 +290,7 @@ void fill(Table<N>& t, const Call& c, int beg, int end) {
         t.size[k] = c.sizes[i];
         t.g_type[k] = (uint8_t)c.types[i];
         t.out_type[k] = (uint8_t)(c.out ? c.out_types[i] : c.types[i]);
-        t.first[k + 1] = t.first[k] + (int)((c.sizes[i] + kChunk - 1) / kChunk);
+        t.first[k + 1] = t.first[k] + (int)((c.sizes[i] + chunk - 1) / chunk);
     }
 }
 
@@ -261,8 +314,27 @@ template <int N>
 cudaError_t run(const Call& c, bool clip, float max_norm, float* norm, double* part, cudaStream_t stream) {
     Table<N> t;
     int parts = 0;
+    int64_t total = 0;
+    for (int i = 0; i < c.count; ++i) total += c.sizes[i];
+    const int chunk = chunk_of(total);
+    if constexpr (N == kFewTensors)
+        if (total <= kSmall) {
+            fill(t, c, 0, c.count, kLeastChunk);
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(kSmallBlocks);
+            cfg.blockDim = dim3(kSmallThreads);
+            cfg.stream = stream;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = kSmallBlocks;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            count_launch();
+            return cudaLaunchKernelEx(&cfg, small_kernel, t, norm, max_norm, clip, c.out == nullptr);
+        }
     for (int beg = 0; beg < c.count; beg += N) {
-        fill(t, c, beg, std::min(c.count, beg + N));
+        fill(t, c, beg, std::min(c.count, beg + N), chunk);
         const int blocks = std::min(t.first[t.tensors], kBlocks);
         if (!blocks) continue;
         squares_kernel<N><<<blocks, kThreads, 0, stream>>>(t, part + parts);
@@ -273,7 +345,7 @@ cudaError_t run(const Call& c, bool clip, float max_norm, float* norm, double* p
     }
     if (!clip || parts == 0) return launch_behind(norm_kernel, 1, stream, (const double*)part, parts, norm);
     for (int beg = (c.count - 1) / N * N; beg >= 0; beg -= N) {
-        if (c.count > N) fill(t, c, beg, std::min(c.count, beg + N));
+        if (c.count > N) fill(t, c, beg, std::min(c.count, beg + N), chunk);
         const int blocks = std::min(t.first[t.tensors], kBlocks);
         if (!blocks) continue;
         const cudaError_t e = launch_behind(scale_kernel<N>, blocks, stream, t, (const double*)part, parts, norm, max_norm, c.out == nullptr);

@@ -359,34 +359,37 @@ cudaError_t launch_short(const Backward& a, cudaStream_t stream) {
     });
 }
 
+template <class TX, class TY, int W, int NV, bool RING, Owner OWNER>
+cudaError_t launch_owners(const Backward& a, cudaStream_t stream) {
+    const int parts = parts_of(a.P), part = part_of(a.P), threads = threads_of(a.P);
+    auto kernel = block_rows_kernel<TX, TY, W, NV, RING, OWNER>;
+    int stages = 0, bytes = 0;
+    if (RING) {
+        static std::atomic<uint64_t> done{0};
+        const cudaError_t e = once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemSm - 4096); });
+        if (e != cudaSuccess) return e;
+        const int stage = part * (int)(sizeof(TX) + sizeof(TY));
+        stages = std::min(kMostStages, (kSmemSm / resident_of(a.P) - 2048) / stage);      // 2 KB: the block's other arrays, and what the driver keeps
+        bytes = stages * stage;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(owners_of(a.N, a.P) * parts));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)parts;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = OWNER == kCluster ? 1 : 0;
+    count_launch();
+    return cudaLaunchKernelEx(&cfg, kernel, a, parts, part, stages);
+}
+
 template <class TX, class TY, int W, int NV, bool RING>
 cudaError_t launch_blocks(const Backward& a, cudaStream_t stream) {
-    const int parts = parts_of(a.P), part = part_of(a.P), threads = threads_of(a.P);
-    auto run = [&](auto kernel) {
-        int stages = 0, bytes = 0;
-        if (RING) {
-            const int stage = part * (int)(sizeof(TX) + sizeof(TY));
-            stages = std::min(kMostStages, (kSmemSm / resident_of(a.P) - 2048) / stage);      // 2 KB: the block's other arrays, and what the driver keeps
-            bytes = stages * stage;
-            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-            if (e != cudaSuccess) return e;
-        }
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(owners_of(a.N, a.P) * parts));
-        cfg.blockDim = dim3((unsigned)threads);
-        cfg.dynamicSmemBytes = (size_t)bytes;
-        cfg.stream = stream;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)parts;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = parts > 1 ? 1 : 0;
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, parts, part, stages);
-        count_launch();
-        return e;
-    };
-    return parts > 1 ? run(block_rows_kernel<TX, TY, W, NV, RING, kCluster>) : run(block_rows_kernel<TX, TY, W, NV, RING, kBlock>);
+    return parts_of(a.P) > 1 ? launch_owners<TX, TY, W, NV, RING, kCluster>(a, stream) : launch_owners<TX, TY, W, NV, RING, kBlock>(a, stream);
 }
 
 template <class TX, class TY>

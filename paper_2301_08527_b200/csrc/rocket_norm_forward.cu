@@ -174,9 +174,13 @@ float unit_of(int P) {
 template <class T, int W, int NV, Owner OWNER, bool HOLD>
 cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream) {
     auto kernel = rows_kernel<T, W, NV, OWNER, HOLD>;
-    int resident = 0;
-    cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, 0);
-    if (e != cudaSuccess) return e;
+    static std::atomic<int> known[1024 / 32 + 1];                        // resident blocks of an SM, by warps; all devices are alike
+    int resident = known[threads / 32].load(std::memory_order_relaxed);
+    if (resident == 0) {
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, 0);
+        if (e != cudaSuccess) return e;
+        known[threads / 32].store(resident, std::memory_order_relaxed);
+    }
     const int64_t owners = OWNER == kWarp ? threads / 32 : 1;            // rows of a block
     const int64_t most = (int64_t)kSms * std::max(resident, 1) / parts;
     const int64_t blocks = std::min(((int64_t)a.N + owners - 1) / owners, std::max<int64_t>(most, 1)) * parts;
@@ -190,9 +194,8 @@ cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = OWNER == kCluster ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, kernel, a, parts, half_of(threads), unit_of(a.P));
     count_launch();
-    return e;
+    return cudaLaunchKernelEx(&cfg, kernel, a, parts, half_of(threads), unit_of(a.P));
 }
 
 template <class T, int W>

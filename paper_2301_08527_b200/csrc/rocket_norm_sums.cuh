@@ -4,6 +4,8 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <atomic>
+#include <cstdint>
 #include <type_traits>
 
 namespace rocket {
@@ -76,6 +78,18 @@ __device__ __forceinline__ float2 row_sums(float2 v, int parts, int rank, int ph
         for (int p = 1; p < parts; ++p) { v.x += share[p].x; v.y += share[p].y; }
     }
     return v;
+}
+
+// Runs set() once for every device that is current at a call (done: a bit for each).
+template <class F>
+inline cudaError_t once_per_device(std::atomic<uint64_t>& done, F&& set) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    const uint64_t bit = uint64_t(1) << (dev & 63);
+    if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_relaxed) & bit))) return e;
+    e = set();
+    if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 inline int round32(int v) { return (v + 31) / 32 * 32; }
