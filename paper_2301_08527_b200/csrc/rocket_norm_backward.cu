@@ -119,6 +119,7 @@ __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
                 }
         }
     }
+    asm volatile("griddepcontrol.launch_dependents;");      // the kernel that adds up the sums waits for this one's end
     if (!a.partial) return;
     // the warps add their sums in turn
     for (int w = 0; w < kThreads / 32; ++w) {
@@ -139,20 +140,23 @@ __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
     for (int i = threadIdx.x; i < 2 * a.P; i += kThreads) out[i] = sums[i];
 }
 
-// RING: the rows come by bulk copies, as many ahead as there are stages; else the threads load them.
-template <class TX, class TY, int W, int NV, bool RING, Owner OWNER>
+// RING: the rows come by bulk copies, as many ahead as there are stages; else the threads load them.  FIT: which words of a thread are within the
+// row needs asking for none of them (2), for its last one (1), for all of them (0).
+template <class TX, class TY, int W, int NV, bool RING, Owner OWNER, int FIT>
 __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward a, int parts, int part, int stages) {
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ __align__(8) uint64_t arrived[kMostStages];
     const int rank = OWNER == kCluster ? blockIdx.x % parts : 0, owner = blockIdx.x / parts, owners = gridDim.x / parts;
     const int beg = rank * part, columns = min(part, a.P - beg), words = columns / W, first = threadIdx.x, step = blockDim.x;
-    auto has = [&](int k) { return first + k * step < words; };
+    const bool last = first + (NV - 1) * step < words;
+    auto has = [&](int k) { return FIT == 2 || (FIT == 1 ? k < NV - 1 || last : first + k * step < words); };
     const uint32_t bars = fast::smem_u32(arrived), rings = fast::smem_u32(ring);
     const int x_bytes = part * (int)sizeof(TX), stage_bytes = x_bytes + part * (int)sizeof(TY);
     const TX* x_from = static_cast<const TX*>(a.x) + beg;
     const TY* y_from = static_cast<const TY*>(a.dy) + beg;
     // a copy's size is a multiple of 16 bytes: the words behind the last such one are loaded by their threads
     const int x_whole = columns * (int)sizeof(TX) / 16 * 16, y_whole = columns * (int)sizeof(TY) / 16 * 16;
+    auto copied = [&](int k, int end_bytes, int whole) { return FIT == 2 || (FIT == 1 && k < NV - 1) || end_bytes <= whole; };
     int64_t to_copy = owner;
     auto copy = [&](int stage) {
         const uint32_t bar = bars + 8u * stage, dst = rings + (uint32_t)(stage * stage_bytes);
@@ -201,9 +205,9 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
                 float x[W], dy[W];
                 if constexpr (RING) {
                     const unsigned char* in = ring + (size_t)stage * stage_bytes;
-                    if ((i + W) * (int)sizeof(TX) <= x_whole) unpack<TX, W>(load_packed<TX, W>(reinterpret_cast<const TX*>(in) + i), x);
+                    if (copied(k, (i + W) * (int)sizeof(TX), x_whole)) unpack<TX, W>(load_packed<TX, W>(reinterpret_cast<const TX*>(in) + i), x);
                     else unpack<TX, W>(load_packed_ro<TX, W>(xs + i), x);
-                    if ((i + W) * (int)sizeof(TY) <= y_whole) unpack<TY, W>(load_packed<TY, W>(reinterpret_cast<const TY*>(in + x_bytes) + i), dy);
+                    if (copied(k, (i + W) * (int)sizeof(TY), y_whole)) unpack<TY, W>(load_packed<TY, W>(reinterpret_cast<const TY*>(in + x_bytes) + i), dy);
                     else unpack<TY, W>(load_packed_ro<TY, W>(ys + i), dy);
                 } else {
                     unpack<TX, W>(load_packed_once<TX, W>(xs + i), x);
@@ -239,6 +243,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
             fast::mbar_wait(bars + 8u * stage, parity);
             if (++stage == stages) { stage = 0; parity ^= 1u; }
         }
+    asm volatile("griddepcontrol.launch_dependents;");
     if (!a.partial) return;
     float* out = a.partial + (int64_t)owner * 2 * a.P + beg;
 #pragma unroll
@@ -253,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
 }
 
 // dg and db from the owners' sums: a block has 32 columns, its warps share the owners.
-constexpr int kSumWarps = 16;
+constexpr int kSumWarps = 32;
 __global__ void __launch_bounds__(kSumWarps * 32) sum_owners_kernel(const float* __restrict__ partial, int owners, int P, void* dgamma, void* dbeta,
                                                                     int w_type) {
     __shared__ float red[2][kSumWarps][32];
@@ -262,7 +267,7 @@ __global__ void __launch_bounds__(kSumWarps * 32) sum_owners_kernel(const float*
     asm volatile("griddepcontrol.wait;" ::: "memory");
     float s = 0.0f, q = 0.0f;
     if (p < P)
-#pragma unroll 4
+#pragma unroll 8
         for (int o = warp; o < owners; o += kSumWarps) {
             const float* from = partial + (int64_t)o * 2 * P + p;
             q += from[0];
@@ -359,10 +364,11 @@ cudaError_t launch_short(const Backward& a, cudaStream_t stream) {
     });
 }
 
-template <class TX, class TY, int W, int NV, bool RING, Owner OWNER>
-cudaError_t launch_owners(const Backward& a, cudaStream_t stream) {
+// owners: of at most so many, how many there are is put here.
+template <class TX, class TY, int W, int NV, bool RING, Owner OWNER, int FIT>
+cudaError_t launch_owners(const Backward& a, int& owners, cudaStream_t stream) {
     const int parts = parts_of(a.P), part = part_of(a.P), threads = threads_of(a.P);
-    auto kernel = block_rows_kernel<TX, TY, W, NV, RING, OWNER>;
+    auto kernel = block_rows_kernel<TX, TY, W, NV, RING, OWNER, FIT>;
     int stages = 0, bytes = 0;
     if (RING) {
         static std::atomic<uint64_t> done{0};
@@ -373,7 +379,7 @@ cudaError_t launch_owners(const Backward& a, cudaStream_t stream) {
         bytes = stages * stage;
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(owners_of(a.N, a.P) * parts));
+    cfg.gridDim = dim3((unsigned)(owners * parts));
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)bytes;
     cfg.stream = stream;
@@ -383,13 +389,32 @@ cudaError_t launch_owners(const Backward& a, cudaStream_t stream) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = OWNER == kCluster ? 1 : 0;
+    if constexpr (OWNER == kCluster) {
+        // not every SM finds partners in its group of SMs: clusters that would have to wait for others to end cost a second round
+        static std::atomic<int> known[kMostParts + 1][kThreads / 32 + 1];
+        int most = 0;
+        const cudaError_t e = active_clusters(known[parts][threads / 32], kernel, cfg, most);
+        if (e != cudaSuccess) return e;
+        owners = std::min(owners, most);
+        cfg.gridDim = dim3((unsigned)(owners * parts));
+    }
     count_launch();
     return cudaLaunchKernelEx(&cfg, kernel, a, parts, part, stages);
 }
 
 template <class TX, class TY, int W, int NV, bool RING>
-cudaError_t launch_blocks(const Backward& a, cudaStream_t stream) {
-    return parts_of(a.P) > 1 ? launch_owners<TX, TY, W, NV, RING, kCluster>(a, stream) : launch_owners<TX, TY, W, NV, RING, kBlock>(a, stream);
+cudaError_t launch_blocks(const Backward& a, int& owners, cudaStream_t stream) {
+    const int parts = parts_of(a.P), part = part_of(a.P), least = a.P - (parts - 1) * part, threads = threads_of(a.P);      // least: the last block's columns
+    auto with_fit = [&](auto fit) {
+        constexpr int FIT = decltype(fit)::value;
+        return parts > 1 ? launch_owners<TX, TY, W, NV, RING, kCluster, FIT>(a, owners, stream) : launch_owners<TX, TY, W, NV, RING, kBlock, FIT>(a, owners, stream);
+    };
+    if constexpr (RING) {
+        const bool whole = least * (int)sizeof(TX) % 16 == 0 && least * (int)sizeof(TY) % 16 == 0;
+        if (least == NV * W * threads && part == least && whole) return with_fit(Int<2>());
+        if (least >= (NV - 1) * W * threads + (whole ? 0 : W)) return with_fit(Int<1>());
+    }
+    return with_fit(Int<0>());
 }
 
 template <class TX, class TY>
@@ -423,6 +448,7 @@ cudaError_t launch_backward(const Backward& args, cudaStream_t stream) {
     // bulk copies begin on 16-byte borders
     const bool ring = packs(a.x, ROCKET_F32, 0, 4) && packs(a.dy, ROCKET_F32, 0, 4) &&
                       (a.N <= 1 || (packs(nullptr, a.x_type, a.x_stride, 16 / float_type_bytes(a.x_type)) && packs(nullptr, a.y_type, a.dy_stride, 16 / float_type_bytes(a.y_type))));
+    int owners = owners_of(a.N, a.P);
     const cudaError_t e = with_float_type(a.x_type, [&](auto* px) {
         return with_float_type(a.y_type, [&](auto* py) {
             using TX = std::remove_pointer_t<decltype(px)>;
@@ -432,9 +458,9 @@ cudaError_t launch_backward(const Backward& args, cudaStream_t stream) {
                 if constexpr (sizeof(TX) == 2 && sizeof(TY) == 2) if (fits(8)) return launch_short<TX, TY, 8>(a, stream);
                 return fits(4) ? launch_short<TX, TY, 4>(a, stream) : launch_short<TX, TY, 1>(a, stream);
             }
-            if constexpr (sizeof(TX) == 2 && sizeof(TY) == 2) if (ring && fits(8)) return launch_blocks<TX, TY, 8, kColumns / 8, true>(a, stream);
-            if (ring && fits(4)) return launch_blocks<TX, TY, 4, kColumns / 4, true>(a, stream);
-            return launch_blocks<TX, TY, 1, kColumns, false>(a, stream);
+            if constexpr (sizeof(TX) == 2 && sizeof(TY) == 2) if (ring && fits(8)) return launch_blocks<TX, TY, 8, kColumns / 8, true>(a, owners, stream);
+            if (ring && fits(4)) return launch_blocks<TX, TY, 4, kColumns / 4, true>(a, owners, stream);
+            return launch_blocks<TX, TY, 1, kColumns, false>(a, owners, stream);
         });
     });
     if (e != cudaSuccess || is_long(a.P) || !a.partial) return e;
@@ -448,7 +474,7 @@ cudaError_t launch_backward(const Backward& args, cudaStream_t stream) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     count_launch();
-    return cudaLaunchKernelEx(&cfg, sum_owners_kernel, (const float*)a.partial, owners_of(a.N, a.P), a.P, a.dgamma, a.dbeta, a.w_type);
+    return cudaLaunchKernelEx(&cfg, sum_owners_kernel, (const float*)a.partial, owners, a.P, a.dgamma, a.dbeta, a.w_type);
 }
 
 }  // namespace norm

@@ -194,6 +194,14 @@ cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = OWNER == kCluster ? 1 : 0;
+    if constexpr (OWNER == kCluster) {
+        // not every SM finds partners in its group of SMs: clusters that would have to wait for others to end cost a second round
+        static std::atomic<int> clusters[kMostParts + 1][1024 / 32 + 1];
+        int at_once = 0;
+        const cudaError_t e = active_clusters(clusters[parts][threads / 32], kernel, cfg, at_once);
+        if (e != cudaSuccess) return e;
+        cfg.gridDim = dim3((unsigned)std::min<int64_t>(blocks, (int64_t)at_once * parts));
+    }
     count_launch();
     return cudaLaunchKernelEx(&cfg, kernel, a, parts, half_of(threads), unit_of(a.P));
 }

@@ -92,6 +92,17 @@ inline cudaError_t once_per_device(std::atomic<uint64_t>& done, F&& set) {
     return e;
 }
 
+// Clusters of `kernel` that run at the same time, asked for once and kept in `known` (all devices are alike).
+template <class K>
+inline cudaError_t active_clusters(std::atomic<int>& known, K kernel, const cudaLaunchConfig_t& cfg, int& clusters) {
+    clusters = known.load(std::memory_order_relaxed);
+    if (clusters > 0) return cudaSuccess;
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+    clusters = std::max(clusters, 1);
+    if (e == cudaSuccess) known.store(clusters, std::memory_order_relaxed);
+    return e;
+}
+
 inline int round32(int v) { return (v + 31) / 32 * 32; }
 
 // row_sum's `half` for a block of this many threads.
