@@ -39,6 +39,25 @@ int owners_of(int N, int P) {
     return std::max(1, (int)std::min<int64_t>(((int64_t)N + rows - 1) / rows, (int64_t)kSms * resident_of(P) / (is_short(P) ? 1 : parts_of(P))));
 }
 
+// Sums of two values over the threads that own a row, the same bits in each.  Each half of a warp goes on with one of the values, which saves
+// nearly half of the shuffles.  Two sets of buffers, taken in turn, make one barrier a row enough.
+template <Owner OWNER>
+__device__ __forceinline__ float2 row_sums(float2 v, int turn) {
+    const int lane = threadIdx.x & 31;
+    const bool upper = lane >= 16;
+    float s = (upper ? v.y : v.x) + __shfl_xor_sync(0xffffffffu, upper ? v.x : v.y, 16);
+    s = add_lanes(s, 8);
+    if constexpr (OWNER != kWarp) {
+        __shared__ float sets[2][2][kThreads / 32];
+        auto& red = sets[turn & 1];
+        const int warps = blockDim.x >> 5, l = lane & 15;
+        if (l == 0) red[lane >> 4][threadIdx.x >> 5] = s;
+        __syncthreads();
+        s = add_lanes(l < warps ? red[lane >> 4][l & (kThreads / 32 - 1)] : 0.0f, 4);
+    }
+    return make_float2(__shfl_sync(0xffffffffu, s, 0), __shfl_sync(0xffffffffu, s, 16));
+}
+
 // One row's work of a thread: xh and u from x and dy, the sums over the row, the sums over the rows.
 template <int W>
 __device__ __forceinline__ void take(const float (&x)[W], const float (&dy)[W], const float (&g)[W], float m, float r, float (&xh)[W], float (&u)[W],
@@ -105,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
                 unpack<TY, W>(cy[k], dy);
                 take<W>(x, dy, g[k], m, r, xh[k], u[k], dg[k], db[k], s);
             }
-        s = row_sums<kWarp>(s, 1, 0, 0);
+        s = row_sums<kWarp>(s, 0);
         if (a.dx) {
             const float c1 = s.x * over_p * r, c2 = s.y * over_p * r;
             TX* __restrict__ dx = static_cast<TX*>(a.dx) + row * a.dx_stride + lane * W;
@@ -146,6 +165,7 @@ template <class TX, class TY, int W, int NV, bool RING, Owner OWNER, int FIT>
 __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward a, int parts, int part, int stages) {
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ __align__(8) uint64_t arrived[kMostStages];
+    __shared__ Exchange exchange;
     const int rank = OWNER == kCluster ? blockIdx.x % parts : 0, owner = blockIdx.x / parts, owners = gridDim.x / parts;
     const int beg = rank * part, columns = min(part, a.P - beg), words = columns / W, first = threadIdx.x, step = blockDim.x;
     const bool last = first + (NV - 1) * step < words;
@@ -180,22 +200,27 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
         for (int k = 0; k < NV; ++k)
             if (has(k)) load_typed<W>(a.gamma, a.w_type, beg + (first + k * step) * W, g[k]);
     // nobody waits on a barrier, or writes to another block's shared memory, before it is there
-    if constexpr (OWNER == kCluster) cg::this_cluster().sync();
-    else __syncthreads();
+    if constexpr (OWNER == kCluster) {
+        exchange.init();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+        __syncthreads();
+    }
     const float over_p = 1.0f / (float)a.P;
-    int stage = 0, phase = 0;
+    int stage = 0, turn = 0;
     uint32_t parity = 0;
     bool ok = true;
     float m = 0.0f, r = 0.0f;
     if (owner < a.N) { m = __ldg(a.mean + owner); r = __ldg(a.rstd + owner); }
-    for (int64_t row = owner; row < a.N; row += owners, ++phase) {
+    for (int64_t row = owner; row < a.N; row += owners, ++turn) {
         float xh[NV][W], u[NV][W];
         float next_m = 0.0f, next_r = 0.0f;
         if (row + owners < a.N) { next_m = __ldg(a.mean + row + owners); next_r = __ldg(a.rstd + row + owners); }
         const TX* xs = x_from + row * a.x_stride;
         const TY* ys = y_from + row * a.dy_stride;
         if constexpr (RING) {
-            ok = ok && fast::mbar_wait(bars + 8u * stage, parity);
+            ok = ok && wait_soon(bars + 8u * stage, parity);
         }
         float2 s = make_float2(ok ? 0.0f : __int_as_float(0x7fc00000), 0.0f);
 #pragma unroll
@@ -217,10 +242,16 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
             }
         if (!ok) dg[0][0] = db[0][0] = s.x;
         // behind the reduction's first barrier everybody has read the row: the next one may come into its place
-        s = row_sums<OWNER>(s, parts, rank, phase);
+        s = row_sums<OWNER>(s, turn);
         if constexpr (RING) {
             if (threadIdx.x == 0 && ok && to_copy < a.N) copy(stage);
             if (++stage == stages) { stage = 0; parity ^= 1u; }
+        }
+        if constexpr (OWNER == kCluster) {
+            const float2* all = exchange.swap(s, parts, rank, turn, ok);
+            s = all[0];
+            for (int p = 1; p < parts; ++p) { s.x += all[p].x; s.y += all[p].y; }
+            if (!ok) s.x = __int_as_float(0x7fc00000);
         }
         if (a.dx) {
             const float c1 = s.x * over_p * r, c2 = s.y * over_p * r;
@@ -243,6 +274,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
             fast::mbar_wait(bars + 8u * stage, parity);
             if (++stage == stages) { stage = 0; parity ^= 1u; }
         }
+    if constexpr (OWNER == kCluster) leave_cluster();
     asm volatile("griddepcontrol.launch_dependents;");
     if (!a.partial) return;
     float* out = a.partial + (int64_t)owner * 2 * a.P + beg;

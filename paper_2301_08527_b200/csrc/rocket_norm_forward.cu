@@ -1,13 +1,13 @@
 // Layer norm forward: m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), y = (x - m) r g + b for every row.
 //
-// Bound: memory.  A row is read once and stays in registers between its two reductions, while its owner's next row is on its
-// way.  The sums are fp32 and safe at any scale.  The first gives a shift next to the mean, the second is of d = x - shift; what
-// is left of the mean, mean(d), comes off the variance and off every value.  For 16-bit rows the shift is rounded to their type,
-// so that d is exact and a constant row gives 0; for fp32 rows the first sum is taken of x - x[0], to the same end.
+// Bound: memory.  A row is read once and stays in registers while its owner's next row is on its way.  All is relative to x0, the
+// row's first value: differences of values far from zero are exact, a constant row gives 0.  A thread takes the mean c of
+// its values and the sum q of their squared distances from c; where sets of values meet, with n, c and q each, the whole has
+// c = sum n c / sum n and q = sum (q + n (c - whole's c)^2).  So the second moment is never a difference of large numbers, and the
+// threads of a block need one barrier, the blocks of a cluster one exchange per row.
 //
 // Who has a row: a warp where it is short, a block, or the blocks of a cluster where rows are few or longer than a block's
-// registers (each block sums its contiguous part, the sums meet in distributed shared memory).  The owners stay and go through
-// the rows in turn.
+// registers.  The owners stay and go through the rows in turn.
 #include <algorithm>
 
 #include "rocket_float_types.cuh"
@@ -19,12 +19,32 @@ namespace rocket {
 namespace norm {
 namespace {
 
-// W values per word, NV words per thread.  HOLD: a thread's values of gamma and beta stay in registers.
-template <class T, int W, int NV, Owner OWNER, bool HOLD>
-__global__ void __launch_bounds__(OWNER == kWarp || HOLD ? 256 : 1024)
-rows_kernel(const Forward a, int parts, int half, float unit) {
+// Where gamma and beta come from: registers, filled once (kHold); loads of a type known at compile time, both being there (kAsFloat,
+// kAsInput: fp32, the input's); loads that ask (kAsk).
+enum Weights { kAsk, kHold, kAsFloat, kAsInput };
+
+constexpr int kMostStages = 8;
+constexpr int kRingThreads = 512;         // most of a block whose rows come by bulk copies; two such blocks share an SM
+constexpr int kSmemSm = 227 * 1024;       // shared memory of an SM
+
+// Blocks of an SM that the registers are cut for.
+constexpr int resident_blocks(Owner owner, Weights weights, int values) {
+    return owner == kWarp ? (values <= 10 ? 4 : values <= 16 ? 3 : 2) : weights == kHold ? 3 : 1;
+}
+
+// RING: a block's next rows, which lie on 16-byte borders, come into shared memory by bulk copies, as many ahead as there are stages; else
+// the threads hold the next one in registers.  A thread that gives up waiting counts as NaN, which makes the row NaN.
+// W values per word, NV words per thread.  FIT: which of a thread's words are within the row needs asking for none (2), for its
+// last (1), for all of them (0).
+template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT, bool RING = false>
+__global__ void __launch_bounds__(OWNER == kWarp || WEIGHTS == kHold ? 256 : RING ? kRingThreads : 1024,
+                                  RING && WEIGHTS != kHold ? 1024 / kRingThreads : resident_blocks(OWNER, WEIGHTS, NV * W))
+rows_kernel(const Forward a, int parts, int stages) {
+    extern __shared__ __align__(16) unsigned char ring[];
+    __shared__ __align__(8) uint64_t arrived[RING ? kMostStages : 1];
     int64_t row, rows;
-    int beg = 0, words = (a.P + W - 1) / W, first, step, rank = 0;
+    int beg = 0, words = a.P / W, first, step, rank = 0;
+    __shared__ Exchange exchange;
     if constexpr (OWNER == kWarp) {
         row = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
         rows = (int64_t)gridDim.x * (blockDim.x >> 5);
@@ -34,89 +54,183 @@ rows_kernel(const Forward a, int parts, int half, float unit) {
         row = blockIdx.x / parts;
         rows = gridDim.x / parts;
         if constexpr (OWNER == kCluster) {
+            exchange.init();
             rank = blockIdx.x % parts;
             const int all = words, from = (int)((int64_t)all * rank / parts);
             beg = from * W;
             words = (int)((int64_t)all * (rank + 1) / parts) - from;
-            cg::this_cluster().sync();             // nobody writes to another block's shared memory before that block runs
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         }
         first = threadIdx.x;
         step = blockDim.x;
     }
-    const int mine = (words - first + step - 1) / step;    // words of this thread: NV, or fewer (a warp's: NV or NV - 1)
-    const int64_t at = beg + (int64_t)first * W;
-    auto has = [&](int k) { return (OWNER == kWarp && k < NV - 1) || k < mine; };
-    Packed<T, W> next[NV] = {};                            // words beyond the row's end stay zeros
+    const bool last = first + (NV - 1) * step < words;
+    auto has = [&](int k) { return FIT == 2 || (FIT == 1 ? k < NV - 1 || last : first + k * step < words); };
+    const int at = beg + first * W;
+    Packed<T, W> next[RING ? 1 : NV];
     float next0 = 0.0f;
-    auto fetch = [&](int64_t n) {
-        const T* __restrict__ x = static_cast<const T*>(a.x) + n * a.x_stride;
+    const T* source = static_cast<const T*>(a.x) + row * a.x_stride;
+    const int64_t source_step = rows * a.x_stride;
+    auto fetch = [&]() {
+        const T* from = source + at;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (has(k)) next[k] = load_packed_once<T, W>(x + at + (int64_t)k * step * W);
-        if constexpr (sizeof(T) == 4) next0 = to_float(x[0]);
+            if (has(k)) next[RING ? 0 : k] = load_packed_once<T, W>(from + k * step * W);
+        next0 = to_float(__ldg(source));
+        source += source_step;
     };
-    float g[HOLD ? NV : 1][W], b[HOLD ? NV : 1][W];
-    auto weights = [&](int k, float (&gk)[W], float (&bk)[W]) {
-#pragma unroll
-        for (int j = 0; j < W; ++j) { gk[j] = 1.0f; bk[j] = 0.0f; }
-        if (a.gamma) load_typed<W>(a.gamma, a.w_type, at + (int64_t)k * step * W, gk);
-        if (a.beta) load_typed<W>(a.beta, a.w_type, at + (int64_t)k * step * W, bk);
+    const uint32_t bars = fast::smem_u32(arrived), rings = fast::smem_u32(ring), row_bytes = (uint32_t)a.P * (uint32_t)sizeof(T);
+    int64_t to_copy = row;
+    auto copy = [&](int stage) {
+        fast::mbar_arrive_expect_tx(bars + 8u * stage, row_bytes);
+        fast::bulk_g2s(rings + (uint32_t)stage * row_bytes, source, row_bytes, bars + 8u * stage);
+        source += source_step;
+        to_copy += rows;
     };
-    if (row < a.N) fetch(row);
-    if constexpr (HOLD)
+    int stage = 0;
+    uint32_t parity = 0;
+    if constexpr (RING) {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < stages; ++i) fast::mbar_init(bars + 8u * i, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            for (int i = 0; i < stages && to_copy < a.N; ++i) copy(i);
+        }
+    } else {
+        if (row < a.N) fetch();
+    }
+    float g[WEIGHTS == kHold ? NV : 1][W], b[WEIGHTS == kHold ? NV : 1][W];
+    if constexpr (WEIGHTS == kHold)
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (has(k)) weights(k, g[k], b[k]);
-    const float over_p = 1.0f / (float)a.P;
-    for (; row < a.N; row += rows) {
-        float f[NV][W];
-        const float x0 = next0;
+        for (int k = 0; k < NV; ++k) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) unpack<T, W>(next[k], f[k]);
-        if (row + rows < a.N) fetch(row + rows);
-        // unit: a power of two of at most 1 / P, so that no sum overflows
-        float s1 = 0.0f;
+            for (int j = 0; j < W; ++j) { g[k][j] = 1.0f; b[k][j] = 0.0f; }
+            if (a.gamma && has(k)) load_typed<W>(a.gamma, a.w_type, at + k * step * W, g[k]);
+            if (a.beta && has(k)) load_typed<W>(a.beta, a.w_type, at + k * step * W, b[k]);
+        }
+    // values of this thread, its warp, its lane's warp, and the block
+    const int n_thread = ((words - first + step - 1) / step) * W;
+    const float n = (float)(words > first ? n_thread : 0), over_n = n > 0.0f ? 1.0f / n : 0.0f;
+    const float n_warp = add_lanes(n, 16), over_warp = n_warp > 0.0f ? 1.0f / n_warp : 0.0f;
+    __shared__ float warp_n[32];
+    float n_lane = 0.0f, over_lane = 0.0f;
+    if constexpr (OWNER != kWarp) {
+        if ((threadIdx.x & 31) == 0) warp_n[threadIdx.x >> 5] = n_warp;
+        __syncthreads();
+        n_lane = (threadIdx.x & 31) < (blockDim.x >> 5) ? warp_n[threadIdx.x & 31] : 0.0f;
+        over_lane = n_lane > 0.0f ? 1.0f / n_lane : 0.0f;
+    }
+    const float over_block = 1.0f / (float)(words * W), over_p = 1.0f / (float)a.P;
+    // the cluster's blocks, one for every eighth lane
+    const int part_lane = threadIdx.x & 7;
+    float n_part = 0.0f, over_part = 0.0f;
+    if (OWNER == kCluster && part_lane < parts) {
+        const int64_t all = a.P / W;
+        n_part = (float)(((int)(all * (part_lane + 1) / parts) - (int)(all * part_lane / parts)) * W);
+        over_part = 1.0f / n_part;
+    }
+    if constexpr (OWNER == kCluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    bool ok = true;
+    for (int turn = 0; row < a.N; row += rows, ++turn) {
+        float f[NV][W], x0 = next0;
+        if constexpr (RING) {
+            ok = ok && wait_soon(bars + 8u * stage, parity);
+            const T* x = reinterpret_cast<const T*>(ring + (size_t)stage * row_bytes);
+            x0 = ok ? to_float(x[0]) : __int_as_float(0x7fc00000);
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (sizeof(T) == 2 || has(k))
+            for (int k = 0; k < NV; ++k)
+                if (has(k)) unpack<T, W>(load_packed<T, W>(x + at + k * step * W), f[k]);
+        } else {
 #pragma unroll
-                for (int j = 0; j < W; ++j) s1 = fmaf(sizeof(T) == 4 ? f[k][j] - x0 : f[k][j], unit, s1);
-        s1 = row_sum<OWNER>(s1, parts, rank, half);
-        const float shift = to_float(from_float<T>(x0 + s1 * (over_p / unit)));
-        float2 s2 = make_float2(0.0f, 0.0f);
+            for (int k = 0; k < NV; ++k)
+                if (has(k)) unpack<T, W>(next[RING ? 0 : k], f[k]);
+            if (row + rows < a.N) fetch();
+        }
+        float s[2] = {0.0f, 0.0f}, q[2] = {0.0f, 0.0f};         // two chains each
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (has(k))
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
-                    f[k][j] -= shift;
-                    s2.x += f[k][j];
-                    s2.y = fmaf(f[k][j], f[k][j], s2.y);
+                    f[k][j] -= x0;
+                    s[(k * W + j) & 1] += f[k][j];
                 }
-        s2 = row_sums<OWNER>(s2, parts, rank, 0);
-        const float rest = s2.x * over_p;
-        const float v = fmaf(-rest, rest, s2.y * over_p), r = rsqrtf((v < 0.0f ? 0.0f : v) + a.eps);      // a NaN stays one
-        const float off = -rest * r;
-        const int64_t out = row * a.y_stride + at;
+        float sum = s[0] + s[1], c = sum * over_n;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (has(k)) {
-                float o[W];
-                if constexpr (HOLD) {
+            if (has(k))
 #pragma unroll
-                    for (int j = 0; j < W; ++j) o[j] = fmaf(fmaf(f[k][j], r, off), g[k][j], b[k][j]);
-                } else {
-                    weights(k, g[0], b[0]);
-#pragma unroll
-                    for (int j = 0; j < W; ++j) o[j] = fmaf(fmaf(f[k][j], r, off), g[0][j], b[0][j]);
+                for (int j = 0; j < W; ++j) {
+                    const float d = f[k][j] - c;
+                    q[(k * W + j) & 1] = fmaf(d, d, q[(k * W + j) & 1]);
                 }
-                store_typed<W>(a.y, a.y_type, out + (int64_t)k * step * W, o);
+        float square = q[0] + q[1];
+        sum = add_lanes(sum, 16);
+        float mean = sum * over_warp, e = c - mean;
+        square = add_lanes(fmaf(n * e, e, square), 16);
+        if constexpr (OWNER != kWarp) {
+            __shared__ float2 sets[2][32];                        // taken in turn: one barrier a row is enough
+            const int lane = threadIdx.x & 31;
+            if (lane == 0) sets[turn & 1][threadIdx.x >> 5] = make_float2(sum, square);
+            __syncthreads();
+            if constexpr (RING) {
+                // everybody has the row in registers: another may come into its place
+                if (threadIdx.x == 0 && ok && to_copy < a.N) copy(stage);
+                if (++stage == stages) { stage = 0; parity ^= 1u; }
             }
+            const float2 of = lane < (int)(blockDim.x >> 5) ? sets[turn & 1][lane] : make_float2(0.0f, 0.0f);
+            sum = add_lanes(of.x, 16);
+            mean = sum * over_block;
+            e = of.x * over_lane - mean;
+            square = add_lanes(fmaf(n_lane * e, e, of.y), 16);
+            if constexpr (OWNER == kCluster) {
+                const float2* all = exchange.swap(make_float2(sum, square), parts, rank, turn, ok);
+                const float2 theirs = part_lane < parts ? all[part_lane] : make_float2(0.0f, 0.0f);
+                mean = add_lanes(theirs.x, 4) * over_p;
+                e = theirs.x * over_part - mean;
+                square = add_lanes(fmaf(n_part * e, e, theirs.y), 4);
+                if (!ok) square = __int_as_float(0x7fc00000);
+            }
+        }
+        const float r = rsqrtf(fmaf(square, over_p, a.eps)), off = -mean * r;
+        auto write = [&](auto* y) {
+            y += row * a.y_stride + at;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (has(k)) {
+                    const int i = at + k * step * W, h = WEIGHTS == kHold ? k : 0;
+                    float o[W];
+                    if constexpr (WEIGHTS == kAsFloat) {
+                        unpack<float, W>(load_packed_ro<float, W>(static_cast<const float*>(a.gamma) + i), g[0]);
+                        unpack<float, W>(load_packed_ro<float, W>(static_cast<const float*>(a.beta) + i), b[0]);
+                    } else if constexpr (WEIGHTS == kAsInput) {
+                        unpack<T, W>(load_packed_ro<T, W>(static_cast<const T*>(a.gamma) + i), g[0]);
+                        unpack<T, W>(load_packed_ro<T, W>(static_cast<const T*>(a.beta) + i), b[0]);
+                    } else if constexpr (WEIGHTS == kAsk) {
+#pragma unroll
+                        for (int j = 0; j < W; ++j) { g[0][j] = 1.0f; b[0][j] = 0.0f; }
+                        if (a.gamma) load_typed<W>(a.gamma, a.w_type, i, g[0]);
+                        if (a.beta) load_typed<W>(a.beta, a.w_type, i, b[0]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < W; ++j) o[j] = fmaf(fmaf(f[k][j], r, off), g[h][j], b[h][j]);
+                    store_packed(y + k * step * W, o);
+                }
+        };
+        if (a.y_type == ROCKET_F32) write(static_cast<float*>(a.y));
+        else if (a.y_type == ROCKET_F16) write(static_cast<__half*>(a.y));
+        else write(static_cast<__nv_bfloat16*>(a.y));
         if (first == 0 && rank == 0) {
-            if (a.mean) a.mean[row] = shift + rest;
+            if (a.mean) a.mean[row] = x0 + mean;
             if (a.rstd) a.rstd[row] = r;
         }
     }
+    // copies that a wait gave up on must not outlive the block
+    if (RING && threadIdx.x == 0 && !ok)
+        for (int i = 0; i < stages; ++i) {
+            fast::mbar_wait(bars + 8u * stage, parity);
+            if (++stage == stages) { stage = 0; parity ^= 1u; }
+        }
+    if constexpr (OWNER == kCluster) leave_cluster();
 }
 
 // Rows longer than the registers of a cluster: a block per row, the row read three times, its sums in double precision.
@@ -165,15 +279,12 @@ __global__ void __launch_bounds__(kLongThreads) long_rows_kernel(const Forward a
     }
 }
 
-// Sum's scale: the largest power of two that is at most 1 / P.
-float unit_of(int P) {
-    int bits = 0;
-    while ((int64_t(1) << bits) < P) ++bits;
-    return ldexpf(1.0f, -bits);
-}
-template <class T, int W, int NV, Owner OWNER, bool HOLD>
+// Shared memory for a block's rows: 2 KB less than its share, for its other arrays and what the driver keeps.
+int ring_bytes(int resident) { return kSmemSm / resident - 2048; }
+
+template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT>
 cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream) {
-    auto kernel = rows_kernel<T, W, NV, OWNER, HOLD>;
+    auto kernel = rows_kernel<T, W, NV, OWNER, WEIGHTS, FIT>;
     static std::atomic<int> known[1024 / 32 + 1];                        // resident blocks of an SM, by warps; all devices are alike
     int resident = known[threads / 32].load(std::memory_order_relaxed);
     if (resident == 0) {
@@ -203,34 +314,81 @@ cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream
         cfg.gridDim = dim3((unsigned)std::min<int64_t>(blocks, (int64_t)at_once * parts));
     }
     count_launch();
-    return cudaLaunchKernelEx(&cfg, kernel, a, parts, half_of(threads), unit_of(a.P));
+    return cudaLaunchKernelEx(&cfg, kernel, a, parts, 0);
+}
+
+// Blocks of `resident` per SM, each with as many stages as there is memory for.
+template <class T, int W, int NV, Weights WEIGHTS, int FIT>
+cudaError_t launch_ring(const Forward& a, int threads, int resident, cudaStream_t stream) {
+    auto kernel = rows_kernel<T, W, NV, kBlock, WEIGHTS, FIT, true>;
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemSm - 4096); });
+    if (e != cudaSuccess) return e;
+    const int row_bytes = a.P * (int)sizeof(T), stages = std::min(kMostStages, ring_bytes(resident) / row_bytes);
+    kernel<<<(unsigned)std::min(a.N, kSms * resident), threads, (size_t)stages * row_bytes, stream>>>(a, 1, stages);
+    count_launch();
+    return cudaGetLastError();
 }
 
 template <class T, int W>
 cudaError_t launch_words(const Forward& a, cudaStream_t stream) {
-    const int words = (a.P + W - 1) / W;
+    const int words = a.P / W;
     constexpr int kWarpWords = W == 1 ? 16 : 32 / W;                // of a lane: rows of up to 512 values, 1,024 in wider words
     if (words <= 32 * kWarpWords)
         return with_int<1, kWarpWords>((words + 31) / 32, [&](auto nv) {
-            return launch<T, W, nv.value, kWarp, nv.value * W <= 16>(a, 256, 1, stream);
+            return launch<T, W, nv.value, kWarp, nv.value * W <= 16 ? kHold : kAsk, 1>(a, 256, 1, stream);
         });
     constexpr int kBlockWords = W == 1 ? 16 : W == 8 ? 3 : 5;       // of a thread
     int parts = 1;
     while (parts < kMostParts && (words > parts * 1024 * kBlockWords || ((int64_t)parts * a.N <= kSms && a.P >= parts * 2048))) parts *= 2;
-    const int part = (words + parts - 1) / parts;
+    const int part = (words + parts - 1) / parts, least = words / parts;      // words of the blocks
     if (part > 1024 * kBlockWords) {
         long_rows_kernel<T><<<(unsigned)a.N, kLongThreads, 0, stream>>>(a);
         count_launch();
         return cudaGetLastError();
     }
-    int nv = (part + 1023) / 1024;
-    while (nv < kBlockWords && (part + nv - 1) / nv > 256 && nv * W < 16) ++nv;
-    return with_int<1, kBlockWords>(nv, [&](auto n) {
-        const int threads = round32((part + n.value - 1) / n.value);
-        if constexpr (n.value * W <= 16) if (parts == 1 && threads <= 256 && a.N > 8 * kSms) return launch<T, W, n.value, kBlock, true>(a, threads, 1, stream);
-        return parts > 1 ? launch<T, W, n.value, kCluster, false>(a, threads, parts, stream)
-                         : launch<T, W, n.value, kBlock, false>(a, threads, 1, stream);
-    });
+    if constexpr (W == 1) {
+        const int nv = part <= 1024 ? 2 : part <= 4096 ? 4 : 16;
+        auto with = [&](auto n) {
+            const int threads = round32((part + n.value - 1) / n.value);
+            return parts > 1 ? launch<T, W, n.value, kCluster, kAsk, 0>(a, threads, parts, stream) : launch<T, W, n.value, kBlock, kAsk, 0>(a, threads, 1, stream);
+        };
+        return nv == 2 ? with(Int<2>()) : nv == 4 ? with(Int<4>()) : with(Int<16>());
+    } else {
+        // rows that a block of 256 threads holds with 16 values each, and enough of them: gamma and beta stay in registers
+        constexpr int kHeld = 16 / W;
+        const int held = round32((words + kHeld - 1) / kHeld);
+        const bool many = parts == 1 && held <= 256 && (kHeld - 1) * held <= words && a.N > 8 * kSms;
+        const bool bulk = parts == 1 && a.P * (int64_t)sizeof(T) % 16 == 0 && packs(a.x, a.x_type, a.N > 1 ? a.x_stride : 0, 16 / (int)sizeof(T));
+        const int resident = std::min(768 / held, 8);
+        if (many && bulk && 2 * a.P * (int64_t)sizeof(T) <= ring_bytes(resident))
+            return words == kHeld * held ? launch_ring<T, W, kHeld, kHold, 2>(a, held, resident, stream) : launch_ring<T, W, kHeld, kHold, 1>(a, held, resident, stream);
+        if (many)
+            return words == kHeld * held ? launch<T, W, kHeld, kBlock, kHold, 2>(a, held, 1, stream) : launch<T, W, kHeld, kBlock, kHold, 1>(a, held, 1, stream);
+        // longer ones, from two rows a block on: up to 40 values of a thread
+        if constexpr (W * sizeof(T) == 16) {
+            constexpr int kLong = 40 / W;
+            const int t = round32((words + kLong - 1) / kLong);
+            if (bulk && t <= kRingThreads && (kLong - 1) * t <= words && a.N >= 4 * kSms && a.P * (int64_t)sizeof(T) <= ring_bytes(2) && a.gamma && a.beta) {
+                if (a.w_type == ROCKET_F32) return launch_ring<T, W, kLong, kAsFloat, 1>(a, t, 2, stream);
+                if constexpr (sizeof(T) == 2) if (a.w_type == a.x_type) return launch_ring<T, W, kLong, kAsInput, 1>(a, t, 2, stream);
+            }
+        }
+        int nv = (part + 1023) / 1024;
+        while (nv < kBlockWords && (part + nv - 1) / nv > 256 && nv * W < 16) ++nv;
+        while (nv > 1 && (nv - 1) * round32((part + nv - 1) / nv) > least) --nv;
+        return with_int<1, kBlockWords>(nv, [&](auto n) {
+            const int threads = round32((part + n.value - 1) / n.value);
+            auto with = [&](auto w) {
+                constexpr Weights WEIGHTS = decltype(w)::value;
+                return parts > 1 ? launch<T, W, n.value, kCluster, WEIGHTS, 1>(a, threads, parts, stream) : launch<T, W, n.value, kBlock, WEIGHTS, 1>(a, threads, 1, stream);
+            };
+            const bool both = a.gamma && a.beta;
+            if (both && a.w_type == ROCKET_F32) return with(std::integral_constant<Weights, kAsFloat>());
+            if constexpr (sizeof(T) == 2) if (both && a.w_type == a.x_type) return with(std::integral_constant<Weights, kAsInput>());
+            return with(std::integral_constant<Weights, kAsk>());
+        });
+    }
 }
 
 }  // namespace
@@ -242,7 +400,7 @@ cudaError_t launch_forward(const Forward& a, cudaStream_t stream) {
             return a.P % W == 0 && packs(a.x, a.x_type, a.N > 1 ? a.x_stride : 0, W) && packs(a.y, a.y_type, a.N > 1 ? a.y_stride : 0, W) &&
                    packs(a.gamma, a.w_type, 0, W) && packs(a.beta, a.w_type, 0, W);
         };
-        if constexpr (sizeof(T) == 2) if (fits(8)) return launch_words<T, 8>(a, stream);
+        if constexpr (sizeof(T) == 2) if (a.y_type != ROCKET_F32 && fits(8)) return launch_words<T, 8>(a, stream);
         if (fits(4)) return launch_words<T, 4>(a, stream);
         return launch_words<T, 1>(a, stream);
     });

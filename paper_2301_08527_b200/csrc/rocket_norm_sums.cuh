@@ -1,25 +1,29 @@
 // Sums over the threads that own a row, shared by the layer norm kernels of both directions.
 #pragma once
 
-#include <cooperative_groups.h>
-
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
 #include <type_traits>
 
+#include "rocket_fast_dev.cuh"
+
 namespace rocket {
 namespace norm {
-
-namespace cg = cooperative_groups;
 
 constexpr int kSms = 148;
 constexpr int kMostParts = 8;             // blocks of a cluster
 
 enum Owner { kWarp, kBlock, kCluster };
 
-// Sums of a value over all threads that own the row, the same bits in each.  The two reductions of a row have buffers of their own,
-// so that one barrier each is enough: a warp that writes for the next row has passed the other's, behind everybody's reads.
+// A bounded wait that does not sleep at first: what it waits for is nearly always there, or about to be.
+__device__ __forceinline__ bool wait_soon(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < 8; ++i)
+        if (fast::mbar_try(bar, parity)) return true;
+    return fast::mbar_wait(bar, parity);
+}
+
+// Sums over the lanes whose numbers differ in the bits from `from` down, the same bits in each.
 __device__ __forceinline__ float add_lanes(float v, int from) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
@@ -27,57 +31,44 @@ __device__ __forceinline__ float add_lanes(float v, int from) {
     return v;
 }
 
-template <Owner OWNER>
-__device__ __forceinline__ float row_sum(float v, int parts, int rank, int half) {
-    v = add_lanes(v, 16);
-    if constexpr (OWNER != kWarp) {
-        __shared__ float red[32];
-        const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-        if (lane == 0) red[threadIdx.x >> 5] = v;
-        __syncthreads();
-        const int l = half ? lane & (2 * half - 1) : 0;                     // 2 half: the warps, rounded up to a power of two
-        v = add_lanes(l < warps ? red[l] : 0.0f, half);
-        if constexpr (OWNER == kCluster) {
-            __shared__ float share[kMostParts];
-            cg::cluster_group cluster = cg::this_cluster();
-            if ((int)threadIdx.x < parts) *cluster.map_shared_rank(&share[rank], threadIdx.x) = v;
-            cluster.sync();
-            v = share[0];
-            for (int p = 1; p < parts; ++p) v += share[p];
+// Two values of every block of a cluster, handed to all of its blocks by stores that count on the receiver's barrier: nothing
+// waits for the rows written meanwhile, as a cluster-wide barrier would.  One exchange per row; with two sets of buffers a block that is
+// ahead writes where nobody reads any more: it has everybody's values of the row before, sent behind the block barrier that follows
+// their reads.
+struct Exchange {
+    float2 share[2][kMostParts];
+    uint64_t bar[2];
+
+    // Behind it, all blocks of the cluster must meet before the first exchange.
+    __device__ __forceinline__ void init() {
+        if (threadIdx.x == 0) {
+            fast::mbar_init(fast::smem_u32(&bar[0]), 1);
+            fast::mbar_init(fast::smem_u32(&bar[1]), 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
     }
-    return v;
-}
 
-// The same of two values: each half of a warp goes on with one of them, which saves nearly half of the shuffles.  A kernel that has this
-// reduction alone gives its rows' numbers as `phase`: with two sets of buffers one barrier a row is enough again.
-template <Owner OWNER>
-__device__ __forceinline__ float2 row_sums(float2 v, int parts, int rank, int phase) {
-    const int lane = threadIdx.x & 31;
-    const bool upper = lane >= 16;
-    float s = (upper ? v.y : v.x) + __shfl_xor_sync(0xffffffffu, upper ? v.x : v.y, 16);
-    s = add_lanes(s, 8);
-    if constexpr (OWNER != kWarp) {
-        __shared__ float reds[2][2][32];
-        auto& red = reds[phase & 1];
-        const int warps = blockDim.x >> 5;
-        if ((lane & 15) == 0) red[lane >> 4][threadIdx.x >> 5] = s;
-        __syncthreads();
-        const int l = lane & 15;
-        s = (l < warps ? red[lane >> 4][l] : 0.0f) + (l + 16 < warps ? red[lane >> 4][l + 16] : 0.0f);
-        s = add_lanes(s, 8);
+    // All threads call it with the block's value v; returns the set of buffers that holds everybody's.  turn: 0, 1, 2 ..  false in ok: a wait
+    // gave up, and nothing is waited for after that.
+    __device__ __forceinline__ const float2* swap(float2 v, int parts, int rank, int turn, bool& ok) {
+        const int set = turn & 1;
+        if (threadIdx.x == 0) fast::mbar_arrive_expect_tx(fast::smem_u32(&bar[set]), (uint32_t)(parts * sizeof(float2)));
+        if ((int)threadIdx.x < parts) {
+            uint32_t to, on;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(fast::smem_u32(&share[set][rank])), "r"((int)threadIdx.x));
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(on) : "r"(fast::smem_u32(&bar[set])), "r"((int)threadIdx.x));
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                         ::"r"(to), "f"(v.x), "f"(v.y), "r"(on) : "memory");
+        }
+        ok = ok && wait_soon(fast::smem_u32(&bar[set]), (uint32_t)((turn >> 1) & 1));
+        return share[set];
     }
-    v = make_float2(__shfl_sync(0xffffffffu, s, 0), __shfl_sync(0xffffffffu, s, 16));
-    if constexpr (OWNER == kCluster) {
-        __shared__ float2 shares[2][kMostParts];
-        auto& share = shares[phase & 1];
-        cg::cluster_group cluster = cg::this_cluster();
-        if ((int)threadIdx.x < parts) *cluster.map_shared_rank(&share[rank], threadIdx.x) = v;
-        cluster.sync();
-        v = share[0];
-        for (int p = 1; p < parts; ++p) { v.x += share[p].x; v.y += share[p].y; }
-    }
-    return v;
+};
+
+// No block of a cluster ends while another may still write to its shared memory.
+__device__ __forceinline__ void leave_cluster() {
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 }
 
 // Runs set() once for every device that is current at a call (done: a bit for each).
@@ -104,13 +95,6 @@ inline cudaError_t active_clusters(std::atomic<int>& known, K kernel, const cuda
 }
 
 inline int round32(int v) { return (v + 31) / 32 * 32; }
-
-// row_sum's `half` for a block of this many threads.
-inline int half_of(int threads) {
-    int half = 0;
-    while (std::max(2 * half, 1) < threads / 32) half = std::max(2 * half, 1);
-    return half;
-}
 
 template <int N> using Int = std::integral_constant<int, N>;
 
