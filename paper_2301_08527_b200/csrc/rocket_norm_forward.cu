@@ -24,32 +24,35 @@ namespace {
 enum Weights { kAsk, kHold, kAsFloat, kAsInput };
 
 constexpr int kMostStages = 8;
-constexpr int kRingThreads = 512;         // most of a block whose rows come by bulk copies; two such blocks share an SM
 constexpr int kSmemSm = 227 * 1024;       // shared memory of an SM
+
+// Threads that hold 32 values of x, gamma and beta each: most of a block, and of one in a cluster.
+constexpr int kHeldValues = 32, kHoldThreads = 128, kHoldClusterThreads = 160;
 
 // Blocks of an SM that the registers are cut for.
 constexpr int resident_blocks(Owner owner, Weights weights, int values) {
-    return owner == kWarp ? (values <= 10 ? 4 : values <= 16 ? 3 : 2) : weights == kHold ? 3 : 1;
+    return owner == kWarp ? (values <= 10 ? 4 : values <= 14 ? 3 : 2) : weights == kHold ? (owner == kCluster ? 3 : 4) : 1;
 }
 
 // RING: a block's next rows, which lie on 16-byte borders, come into shared memory by bulk copies, as many ahead as there are stages; else
 // the threads hold the next one in registers.  A thread that gives up waiting counts as NaN, which makes the row NaN.
 // W values per word, NV words per thread.  FIT: which of a thread's words are within the row needs asking for none (2), for its
 // last (1), for all of them (0).
-template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT, bool RING = false>
-__global__ void __launch_bounds__(OWNER == kWarp || WEIGHTS == kHold ? 256 : RING ? kRingThreads : 1024,
-                                  RING && WEIGHTS != kHold ? 1024 / kRingThreads : resident_blocks(OWNER, WEIGHTS, NV * W))
-rows_kernel(const Forward a, int parts, int stages) {
+// LANES: of a warp that share a row; a warp has 32 / LANES rows at a time.
+template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT, bool RING = false, int LANES = 32>
+__global__ void __launch_bounds__(OWNER == kWarp ? 256 : WEIGHTS == kHold ? (OWNER == kCluster ? kHoldClusterThreads : kHoldThreads) : 1024,
+                                  resident_blocks(OWNER, WEIGHTS, NV * W))
+rows_kernel(const Forward a, int parts, int stages, int stage_words) {
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ __align__(8) uint64_t arrived[RING ? kMostStages : 1];
     int64_t row, rows;
     int beg = 0, words = a.P / W, first, step, rank = 0;
     __shared__ Exchange exchange;
     if constexpr (OWNER == kWarp) {
-        row = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-        rows = (int64_t)gridDim.x * (blockDim.x >> 5);
-        first = threadIdx.x & 31;
-        step = 32;
+        row = (int64_t)blockIdx.x * (blockDim.x / LANES) + (threadIdx.x >> 5) * (32 / LANES);      // the warp's first; its lanes' below
+        rows = (int64_t)gridDim.x * (blockDim.x / LANES);
+        first = threadIdx.x & (LANES - 1);
+        step = LANES;
     } else {
         row = blockIdx.x / parts;
         rows = gridDim.x / parts;
@@ -69,21 +72,23 @@ rows_kernel(const Forward a, int parts, int stages) {
     const int at = beg + first * W;
     Packed<T, W> next[RING ? 1 : NV];
     float next0 = 0.0f;
-    const T* source = static_cast<const T*>(a.x) + row * a.x_stride;
+    const int ahead = OWNER == kWarp ? (threadIdx.x & 31) / LANES : 0;
+    const T* source = static_cast<const T*>(a.x) + (row + ahead) * a.x_stride;
     const int64_t source_step = rows * a.x_stride;
-    auto fetch = [&]() {
+    auto fetch = [&](int64_t n) {
         const T* from = source + at;
+        if (LANES < 32 && n + ahead >= a.N) return;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (has(k)) next[RING ? 0 : k] = load_packed_once<T, W>(from + k * step * W);
         next0 = to_float(__ldg(source));
         source += source_step;
     };
-    const uint32_t bars = fast::smem_u32(arrived), rings = fast::smem_u32(ring), row_bytes = (uint32_t)a.P * (uint32_t)sizeof(T);
+    const uint32_t bars = fast::smem_u32(arrived), rings = fast::smem_u32(ring), row_bytes = (uint32_t)(words * W * (int)sizeof(T)), stage_bytes = (uint32_t)stage_words * (W * sizeof(T));
     int64_t to_copy = row;
     auto copy = [&](int stage) {
         fast::mbar_arrive_expect_tx(bars + 8u * stage, row_bytes);
-        fast::bulk_g2s(rings + (uint32_t)stage * row_bytes, source, row_bytes, bars + 8u * stage);
+        fast::bulk_g2s(rings + (uint32_t)stage * stage_bytes, source + beg, row_bytes, bars + 8u * stage);
         source += source_step;
         to_copy += rows;
     };
@@ -95,8 +100,9 @@ rows_kernel(const Forward a, int parts, int stages) {
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             for (int i = 0; i < stages && to_copy < a.N; ++i) copy(i);
         }
+        if (OWNER == kCluster && row < a.N) next0 = to_float(__ldg(static_cast<const T*>(a.x) + row * a.x_stride));
     } else {
-        if (row < a.N) fetch();
+        if (row < a.N) fetch(row);
     }
     float g[WEIGHTS == kHold ? NV : 1][W], b[WEIGHTS == kHold ? NV : 1][W];
     if constexpr (WEIGHTS == kHold)
@@ -110,7 +116,7 @@ rows_kernel(const Forward a, int parts, int stages) {
     // values of this thread, its warp, its lane's warp, and the block
     const int n_thread = ((words - first + step - 1) / step) * W;
     const float n = (float)(words > first ? n_thread : 0), over_n = n > 0.0f ? 1.0f / n : 0.0f;
-    const float n_warp = add_lanes(n, 16), over_warp = n_warp > 0.0f ? 1.0f / n_warp : 0.0f;
+    const float n_warp = add_lanes(n, LANES / 2), over_warp = n_warp > 0.0f ? 1.0f / n_warp : 0.0f;
     __shared__ float warp_n[32];
     float n_lane = 0.0f, over_lane = 0.0f;
     if constexpr (OWNER != kWarp) {
@@ -134,16 +140,22 @@ rows_kernel(const Forward a, int parts, int stages) {
         float f[NV][W], x0 = next0;
         if constexpr (RING) {
             ok = ok && wait_soon(bars + 8u * stage, parity);
-            const T* x = reinterpret_cast<const T*>(ring + (size_t)stage * row_bytes);
-            x0 = ok ? to_float(x[0]) : __int_as_float(0x7fc00000);
+            const T* x = reinterpret_cast<const T*>(ring + (size_t)stage * stage_bytes);
+            if constexpr (OWNER == kCluster) {
+                x0 = next0;
+                if (row + rows < a.N) next0 = to_float(__ldg(static_cast<const T*>(a.x) + (row + rows) * a.x_stride));
+            } else {
+                x0 = to_float(x[0]);
+            }
+            if (!ok) x0 = __int_as_float(0x7fc00000);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
-                if (has(k)) unpack<T, W>(load_packed<T, W>(x + at + k * step * W), f[k]);
+                if (has(k)) unpack<T, W>(load_packed<T, W>(x + (first + k * step) * W), f[k]);
         } else {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 if (has(k)) unpack<T, W>(next[RING ? 0 : k], f[k]);
-            if (row + rows < a.N) fetch();
+            if (row + rows < a.N) fetch(row + rows);
         }
         float s[2] = {0.0f, 0.0f}, q[2] = {0.0f, 0.0f};         // two chains each
 #pragma unroll
@@ -164,9 +176,9 @@ rows_kernel(const Forward a, int parts, int stages) {
                     q[(k * W + j) & 1] = fmaf(d, d, q[(k * W + j) & 1]);
                 }
         float square = q[0] + q[1];
-        sum = add_lanes(sum, 16);
+        sum = add_lanes(sum, LANES / 2);
         float mean = sum * over_warp, e = c - mean;
-        square = add_lanes(fmaf(n * e, e, square), 16);
+        square = add_lanes(fmaf(n * e, e, square), LANES / 2);
         if constexpr (OWNER != kWarp) {
             __shared__ float2 sets[2][32];                        // taken in turn: one barrier a row is enough
             const int lane = threadIdx.x & 31;
@@ -193,7 +205,7 @@ rows_kernel(const Forward a, int parts, int stages) {
         }
         const float r = rsqrtf(fmaf(square, over_p, a.eps)), off = -mean * r;
         auto write = [&](auto* y) {
-            y += row * a.y_stride + at;
+            y += (row + ahead) * a.y_stride + at;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 if (has(k)) {
@@ -216,12 +228,13 @@ rows_kernel(const Forward a, int parts, int stages) {
                     store_packed(y + k * step * W, o);
                 }
         };
+        if (LANES < 32 && row + ahead >= a.N) break;              // the warp's last turn
         if (a.y_type == ROCKET_F32) write(static_cast<float*>(a.y));
         else if (a.y_type == ROCKET_F16) write(static_cast<__half*>(a.y));
         else write(static_cast<__nv_bfloat16*>(a.y));
         if (first == 0 && rank == 0) {
-            if (a.mean) a.mean[row] = x0 + mean;
-            if (a.rstd) a.rstd[row] = r;
+            if (a.mean) a.mean[row + ahead] = x0 + mean;
+            if (a.rstd) a.rstd[row + ahead] = r;
         }
     }
     // copies that a wait gave up on must not outlive the block
@@ -282,9 +295,9 @@ __global__ void __launch_bounds__(kLongThreads) long_rows_kernel(const Forward a
 // Shared memory for a block's rows: 2 KB less than its share, for its other arrays and what the driver keeps.
 int ring_bytes(int resident) { return kSmemSm / resident - 2048; }
 
-template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT>
+template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT, int LANES = 32>
 cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream) {
-    auto kernel = rows_kernel<T, W, NV, OWNER, WEIGHTS, FIT>;
+    auto kernel = rows_kernel<T, W, NV, OWNER, WEIGHTS, FIT, false, LANES>;
     static std::atomic<int> known[1024 / 32 + 1];                        // resident blocks of an SM, by warps; all devices are alike
     int resident = known[threads / 32].load(std::memory_order_relaxed);
     if (resident == 0) {
@@ -292,7 +305,7 @@ cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream
         if (e != cudaSuccess) return e;
         known[threads / 32].store(resident, std::memory_order_relaxed);
     }
-    const int64_t owners = OWNER == kWarp ? threads / 32 : 1;            // rows of a block
+    const int64_t owners = OWNER == kWarp ? threads / LANES : 1;            // rows of a block
     const int64_t most = (int64_t)kSms * std::max(resident, 1) / parts;
     const int64_t blocks = std::min(((int64_t)a.N + owners - 1) / owners, std::max<int64_t>(most, 1)) * parts;
     cudaLaunchConfig_t cfg = {};
@@ -314,28 +327,52 @@ cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream
         cfg.gridDim = dim3((unsigned)std::min<int64_t>(blocks, (int64_t)at_once * parts));
     }
     count_launch();
-    return cudaLaunchKernelEx(&cfg, kernel, a, parts, 0);
+    return cudaLaunchKernelEx(&cfg, kernel, a, parts, 0, 0);
 }
 
 // Blocks of `resident` per SM, each with as many stages as there is memory for.
-template <class T, int W, int NV, Weights WEIGHTS, int FIT>
-cudaError_t launch_ring(const Forward& a, int threads, int resident, cudaStream_t stream) {
-    auto kernel = rows_kernel<T, W, NV, kBlock, WEIGHTS, FIT, true>;
+template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT>
+cudaError_t launch_ring(const Forward& a, int threads, int parts, int resident, cudaStream_t stream) {
+    auto kernel = rows_kernel<T, W, NV, OWNER, WEIGHTS, FIT, true>;
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemSm - 4096); });
+    cudaError_t e = once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemSm - 4096); });
     if (e != cudaSuccess) return e;
-    const int row_bytes = a.P * (int)sizeof(T), stages = std::min(kMostStages, ring_bytes(resident) / row_bytes);
-    kernel<<<(unsigned)std::min(a.N, kSms * resident), threads, (size_t)stages * row_bytes, stream>>>(a, 1, stages);
+    const int stage_words = (a.P / W + parts - 1) / parts, stage_bytes = stage_words * W * (int)sizeof(T);
+    const int stages = std::min(kMostStages, ring_bytes(resident) / stage_bytes);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(std::min(a.N, kSms * resident / parts) * parts));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)stages * stage_bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)parts;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = OWNER == kCluster ? 1 : 0;
+    if constexpr (OWNER == kCluster) {
+        static std::atomic<int> clusters[kMostParts + 1][1024 / 32 + 1];
+        int at_once = 0;
+        e = active_clusters(clusters[parts][threads / 32], kernel, cfg, at_once);
+        if (e != cudaSuccess) return e;
+        cfg.gridDim = dim3((unsigned)(std::min(a.N, at_once) * parts));
+    }
     count_launch();
-    return cudaGetLastError();
+    return cudaLaunchKernelEx(&cfg, kernel, a, parts, stages, stage_words);
 }
 
 template <class T, int W>
 cudaError_t launch_words(const Forward& a, cudaStream_t stream) {
     const int words = a.P / W;
-    constexpr int kWarpWords = W == 1 ? 16 : 32 / W;                // of a lane: rows of up to 512 values, 1,024 in wider words
-    if (words <= 32 * kWarpWords)
-        return with_int<1, kWarpWords>((words + 31) / 32, [&](auto nv) {
+    // Short rows: as few lanes of a warp as hold the row in up to 16 values each (up to 20 in 16 lanes, 32 in 32), since half of a warp's work
+    // would else be the sums' shuffles.
+    constexpr int kMost = W == 1 ? 16 : 32 / W, kFew = 16 / W, kMiddle = W == 1 ? 20 : 16 / W;
+    if (words <= 8 * kFew)
+        return with_int<1, kFew>((words + 7) / 8, [&](auto nv) { return launch<T, W, nv.value, kWarp, kHold, 1, 8>(a, 256, 1, stream); });
+    if (words <= 16 * kMiddle)
+        return with_int<kFew / 2 + 1, kMiddle>((words + 15) / 16, [&](auto nv) { return launch<T, W, nv.value, kWarp, kHold, 1, 16>(a, 256, 1, stream); });
+    if (words <= 32 * kMost)
+        return with_int<kMiddle / 2 + 1, kMost>((words + 31) / 32, [&](auto nv) {
             return launch<T, W, nv.value, kWarp, nv.value * W <= 16 ? kHold : kAsk, 1>(a, 256, 1, stream);
         });
     constexpr int kBlockWords = W == 1 ? 16 : W == 8 ? 3 : 5;       // of a thread
@@ -355,24 +392,22 @@ cudaError_t launch_words(const Forward& a, cudaStream_t stream) {
         };
         return nv == 2 ? with(Int<2>()) : nv == 4 ? with(Int<4>()) : with(Int<16>());
     } else {
-        // rows that a block of 256 threads holds with 16 values each, and enough of them: gamma and beta stay in registers
-        constexpr int kHeld = 16 / W;
+        // Enough rows: gamma and beta stay in registers, in a block where they fit, else in a cluster.
+        constexpr int kHeld = kHeldValues / W;
+        const bool bulk = a.P * (int64_t)sizeof(T) % 16 == 0 && packs(a.x, a.x_type, a.N > 1 ? a.x_stride : 0, 16 / (int)sizeof(T));
         const int held = round32((words + kHeld - 1) / kHeld);
-        const bool many = parts == 1 && held <= 256 && (kHeld - 1) * held <= words && a.N > 8 * kSms;
-        const bool bulk = parts == 1 && a.P * (int64_t)sizeof(T) % 16 == 0 && packs(a.x, a.x_type, a.N > 1 ? a.x_stride : 0, 16 / (int)sizeof(T));
-        const int resident = std::min(768 / held, 8);
-        if (many && bulk && 2 * a.P * (int64_t)sizeof(T) <= ring_bytes(resident))
-            return words == kHeld * held ? launch_ring<T, W, kHeld, kHold, 2>(a, held, resident, stream) : launch_ring<T, W, kHeld, kHold, 1>(a, held, resident, stream);
-        if (many)
-            return words == kHeld * held ? launch<T, W, kHeld, kBlock, kHold, 2>(a, held, 1, stream) : launch<T, W, kHeld, kBlock, kHold, 1>(a, held, 1, stream);
-        // longer ones, from two rows a block on: up to 40 values of a thread
+        if (held <= kHoldThreads && (kHeld - 1) * held <= words && a.N > 8 * kSms) {
+            const int resident = std::min(512 / held, 8);
+            if constexpr (W * sizeof(T) == 16) if (bulk)
+                return words == kHeld * held ? launch_ring<T, W, kHeld, kBlock, kHold, 2>(a, held, 1, resident, stream)
+                                             : launch_ring<T, W, kHeld, kBlock, kHold, 1>(a, held, 1, resident, stream);
+            return launch<T, W, kHeld, kBlock, kHold, 1>(a, held, 1, stream);
+        }
         if constexpr (W * sizeof(T) == 16) {
-            constexpr int kLong = 40 / W;
-            const int t = round32((words + kLong - 1) / kLong);
-            if (bulk && t <= kRingThreads && (kLong - 1) * t <= words && a.N >= 4 * kSms && a.P * (int64_t)sizeof(T) <= ring_bytes(2) && a.gamma && a.beta) {
-                if (a.w_type == ROCKET_F32) return launch_ring<T, W, kLong, kAsFloat, 1>(a, t, 2, stream);
-                if constexpr (sizeof(T) == 2) if (a.w_type == a.x_type) return launch_ring<T, W, kLong, kAsInput, 1>(a, t, 2, stream);
-            }
+            const int blocks = (words + kHeld * kHoldClusterThreads - 1) / (kHeld * kHoldClusterThreads);
+            const int most = (words + blocks - 1) / blocks, fewest = words / blocks, threads = round32((most + kHeld - 1) / kHeld);
+            if (bulk && blocks > 1 && blocks <= kMostParts && (kHeld - 1) * threads <= fewest && (int64_t)a.N * blocks >= 2 * kSms)
+                return launch_ring<T, W, kHeld, kCluster, kHold, 1>(a, threads, blocks, std::min(512 / threads, 4), stream);
         }
         int nv = (part + 1023) / 1024;
         while (nv < kBlockWords && (part + nv - 1) / nv > 256 && nv * W < 16) ++nv;
