@@ -440,12 +440,13 @@ def _types():
 
 def _on_device(call, device, where):
     """Runs call(stream) with `device` current, on that device's current stream."""
-    index = device.index
-    if index == _current_device():
-        _check(call(_current_stream()), where)
+    if device.index == _current_device():
+        status = call(_current_stream())
     else:
-        with _torch.cuda.device(index):
-            _check(call(_current_stream()), where)
+        with _torch.cuda.device(device.index):
+            status = call(_current_stream())
+    if status:
+        raise RocketError(status, where)
 
 
 def _rows(t, name, shape=None, device=None, dtype=None):
@@ -454,26 +455,24 @@ def _rows(t, name, shape=None, device=None, dtype=None):
     try:
         code = _types().get(t.dtype)
         if code is None or not t.is_cuda:
-            raise TypeError("%s must be a CUDA tensor of float32, float16 or bfloat16" % name)
+            raise AttributeError
     except AttributeError:
         raise TypeError("%s must be a CUDA tensor of float32, float16 or bfloat16" % name) from None
     got = t.shape
-    if shape is not None and got != shape:
-        raise ValueError("%s must have the shape %s" % (name, tuple(shape)))
-    if dtype is not None and t.dtype is not dtype:
-        raise TypeError("%s must be of dtype %s" % (name, dtype))
-    if device is not None and t.device != device:
-        raise ValueError("%s is on another device" % name)
+    if shape is not None:
+        if got != shape:
+            raise ValueError("%s must have the shape %s" % (name, tuple(shape)))
+        if t.device != device:
+            raise ValueError("%s is on another device" % name)
+        if dtype is not None and t.dtype is not dtype:
+            raise TypeError("%s must be of dtype %s" % (name, dtype))
     if len(got) == 2:
         N, P = got
-        stride, step = t.stride()
-        if N > 1 and not t.is_contiguous():
-            if (P > 1 and step != 1) or stride < 0:
+        stride = P
+        if not t.is_contiguous():
+            stride, step = t.stride()
+            if P > 1 and step != 1:
                 raise TypeError("%s must have the values of a row next to one another" % name)
-        elif P > 1 and step != 1:
-            raise TypeError("%s must have the values of a row next to one another" % name)
-        else:
-            stride = max(stride, P)
     else:
         if not got or not t.is_contiguous():
             raise TypeError("%s must be contiguous, or have two dimensions" % name)
@@ -482,6 +481,13 @@ def _rows(t, name, shape=None, device=None, dtype=None):
     if P < 1 or N > 0x7fffffff or P > 0x7fffffff:
         raise ValueError("%s must have rows of at least one value, and at most 2^31 - 1 rows and values per row" % name)
     return t.data_ptr(), code, stride, N, P
+
+
+def _like(t, dtype):
+    """A new contiguous tensor of t's shape, of dtype or t's type."""
+    if t.is_contiguous():
+        return _torch.empty_like(t) if dtype is None else _torch.empty_like(t, dtype=dtype)
+    return t.new_empty(t.shape, dtype=dtype)
 
 
 def _vector(t, n, name, device, dtype=None):
@@ -505,28 +511,34 @@ def rocket_layer_norm(feat, gamma=None, beta=None, eps=1e-5, out=None, out_dtype
     type, or None.  Returns (out, mean, rstd), the statistics fp32, one per row, or None without want_stats."""
     torch = _t()
     x, xt, xs, N, P = _rows(feat, "feat")
-    device, shape = feat.device, feat.shape
-    y = out
+    device, y = feat.device, out
     if y is not None:
-        yp, yt, ys, _, _ = _rows(y, "out", shape, device, out_dtype)
+        yp, yt, ys, _, _ = _rows(y, "out", feat.shape, device, out_dtype)
     else:
-        y = feat.new_empty(shape) if out_dtype is None else feat.new_empty(shape, dtype=out_dtype)
-        yp, yt, ys = y.data_ptr(), _types().get(y.dtype), P
+        y = _like(feat, out_dtype)
+        yp, yt, ys = y.data_ptr(), _float_types.get(y.dtype), P
         if yt is None:
             raise TypeError("out_dtype must be float32, float16 or bfloat16")
-    g, wt = _vector(gamma, P, "gamma", device)
-    b, bt = _vector(beta, P, "beta", device)
-    if wt is None:
-        wt = bt if bt is not None else 0
-    elif bt is not None and wt != bt:
-        raise TypeError("gamma and beta must be of one dtype")
-    mean, rstd = mean_out, rstd_out
-    if want_stats and mean is None:
-        mean = feat.new_empty(shape[:-1], dtype=torch.float32)
-    if want_stats and rstd is None:
+    g = b = None
+    wt = 0
+    if gamma is not None:
+        g, wt = _vector(gamma, P, "gamma", device)
+    if beta is not None:
+        b, bt = _vector(beta, P, "beta", device)
+        if g is not None and wt != bt:
+            raise TypeError("gamma and beta must be of one dtype")
+        wt = bt
+    mean, rstd, mp, rp = mean_out, rstd_out, None, None
+    if mean is not None:
+        mp = _vector(mean, N, "mean_out", device, torch.float32)[0]
+    elif want_stats:
+        mean = torch.empty(N if feat.dim() == 2 else feat.shape[:-1], dtype=torch.float32, device=device)
+        mp = mean.data_ptr()
+    if rstd is not None:
+        rp = _vector(rstd, N, "rstd_out", device, torch.float32)[0]
+    elif want_stats:
         rstd = torch.empty_like(mean)
-    mp = _vector(mean, N, "mean_out", device, torch.float32)[0]
-    rp = _vector(rstd, N, "rstd_out", device, torch.float32)[0]
+        rp = rstd.data_ptr()
     fn = (_lib or load_library()).rocket_layer_norm
     _on_device(lambda s: fn(x, xt, xs, N, P, g, b, wt, eps, yp, yt, ys, mp, rp, s), device, "rocket_layer_norm")
     return y, mean, rstd
@@ -537,40 +549,51 @@ def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dg
     """Gradients of sum(dy * rocket_layer_norm(feat)) for feat, gamma and beta, from the statistics of the forward pass.
     Returns (dx of feat's type, dgamma, dbeta of gamma's type or weight_dtype); what is not wanted is None."""
     torch = _t()
+    f32 = torch.float32
     x, xt, xs, N, P = _rows(feat, "feat")
-    device, shape = feat.device, feat.shape
-    d, yt, ds, _, _ = _rows(dy, "dy", shape, device)
-    mp = _vector(mean, N, "mean", device, torch.float32)[0]
-    rp = _vector(rstd, N, "rstd", device, torch.float32)[0]
+    device = feat.device
+    d, yt, ds, _, _ = _rows(dy, "dy", feat.shape, device)
+    mp = _vector(mean, N, "mean", device, f32)[0]
+    rp = _vector(rstd, N, "rstd", device, f32)[0]
     if mp is None or rp is None:
         raise TypeError("mean and rstd must be the statistics of the forward pass")
-    g, wt = _vector(gamma, P, "gamma", device)
-    if weight_dtype is None:
-        weight_dtype = gamma.dtype if gamma is not None else dgamma_out.dtype if dgamma_out is not None else \
-            dbeta_out.dtype if dbeta_out is not None else torch.float32
-    elif gamma is not None and gamma.dtype is not weight_dtype:
-        raise TypeError("weight_dtype must be gamma's")
-    if wt is None:
-        wt = _types().get(weight_dtype)
+    g = wt = None
+    if gamma is not None:
+        g, wt = _vector(gamma, P, "gamma", device)
+        if weight_dtype is None:
+            weight_dtype = gamma.dtype
+        elif weight_dtype is not gamma.dtype:
+            raise TypeError("weight_dtype must be gamma's")
+    else:
+        if weight_dtype is None:
+            weight_dtype = dgamma_out.dtype if dgamma_out is not None else dbeta_out.dtype if dbeta_out is not None else f32
+        wt = _float_types.get(weight_dtype)
         if wt is None:
             raise TypeError("weight_dtype must be float32, float16 or bfloat16")
     dx, dg, db = dx_out, dgamma_out, dbeta_out
-    dxp, dxs = None, 0
+    dxp, dgp, dbp, dxs = None, None, None, P
     if dx is not None:
-        dxp, _, dxs, _, _ = _rows(dx, "dx_out", shape, device, feat.dtype)
+        dxp, _, dxs, _, _ = _rows(dx, "dx_out", feat.shape, device, feat.dtype)
     elif want_dx:
-        dx = feat.new_empty(shape)
-        dxp, dxs = dx.data_ptr(), P
-    if want_weights and dg is None:
-        dg = feat.new_empty((P,), dtype=weight_dtype) if gamma is None else torch.empty_like(gamma)
-    if want_weights and db is None:
-        db = torch.empty_like(dg)
-    dgp = _vector(dg, P, "dgamma_out", device, weight_dtype)[0]
-    dbp = _vector(db, P, "dbeta_out", device, weight_dtype)[0]
+        dx = _like(feat, None)
+        dxp = dx.data_ptr()
+    if dg is not None:
+        dgp = _vector(dg, P, "dgamma_out", device, weight_dtype)[0]
+    elif want_weights:
+        dg = torch.empty(P, dtype=weight_dtype, device=device)
+        dgp = dg.data_ptr()
+    if db is not None:
+        dbp = _vector(db, P, "dbeta_out", device, weight_dtype)[0]
+    elif want_weights:
+        db = torch.empty(P, dtype=weight_dtype, device=device)
+        dbp = db.data_ptr()
     lib = _lib or load_library()
-    need = max(lib.rocket_layer_norm_backward_workspace(N, P), 0) if dg is not None or db is not None else 0
-    ws = mean.new_empty(need // 4) if need else None
-    wp = ws.data_ptr() if need else None
+    need, wp = 0, None
+    if dgp or dbp:
+        need = lib.rocket_layer_norm_backward_workspace(N, P)
+        if need > 0:
+            ws = torch.empty(need // 4, dtype=f32, device=device)
+            wp = ws.data_ptr()
     fn = lib.rocket_layer_norm_backward
     _on_device(lambda s: fn(d, yt, ds, x, xt, xs, N, P, g, wt, mp, rp, dxp, dxs, dgp, dbp, wp, need, s), device,
                "rocket_layer_norm_backward")
@@ -619,14 +642,17 @@ def _address(a):
 
 
 def _norm_buffers(lib, count, grads, norm_out):
-    torch = _t()
-    norm = norm_out
-    if norm is None:
-        norm = grads[0].new_empty(1, dtype=torch.float32) if count else torch.empty(1, dtype=torch.float32, device="cuda")
-    np_ = _vector(norm, 1, "norm_out", grads[0].device if count else norm.device, torch.float32)[0]
+    torch = _torch
+    f32 = torch.float32
+    device = grads[0].device if count else norm_out.device if norm_out is not None else torch.device("cuda", _current_device())
+    if norm_out is not None:
+        norm, np_ = norm_out, _vector(norm_out, 1, "norm_out", device, f32)[0]
+    else:
+        norm = torch.empty(1, dtype=f32, device=device)
+        np_ = norm.data_ptr()
     need = lib.rocket_grad_norm_workspace(count)
-    ws = norm.new_empty(need // 4)
-    return ws, ws.data_ptr(), need, norm, np_
+    ws = torch.empty(need // 4, dtype=f32, device=device)
+    return ws, ws.data_ptr(), need, norm, np_, device
 
 
 def rocket_grad_norm(grads, norm_out=None):
@@ -634,9 +660,9 @@ def rocket_grad_norm(grads, norm_out=None):
     device).  Returns it as a [1] float32 tensor."""
     lib = _lib or load_library()
     n, ptrs, sizes, codes, _, _ = _tensor_list(grads, "grads")
-    ws, wp, need, norm, np_ = _norm_buffers(lib, n, grads, norm_out)
+    ws, wp, need, norm, np_, device = _norm_buffers(lib, n, grads, norm_out)
     p, z, c = _address(ptrs), _address(sizes), _address(codes)
-    _on_device(lambda s: lib.rocket_grad_norm(n, p, z, c, np_, wp, need, s), norm.device, "rocket_grad_norm")
+    _on_device(lambda s: lib.rocket_grad_norm(n, p, z, c, np_, wp, need, s), device, "rocket_grad_norm")
     return norm
 
 
@@ -654,9 +680,9 @@ def rocket_clip_grad_norm(grads, max_norm, out=None, norm_out=None):
         if not (contiguous and out_contiguous) and any(
                 a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
             raise ValueError("out must have the shapes and strides of the gradients")
-    ws, wp, need, norm, np_ = _norm_buffers(lib, n, grads, norm_out)
+    ws, wp, need, norm, np_, device = _norm_buffers(lib, n, grads, norm_out)
     p, z, c, o, oc = _address(ptrs), _address(sizes), _address(codes), _address(outs), _address(out_codes)
-    _on_device(lambda s: lib.rocket_clip_grad_norm(n, p, z, c, o, oc, max_norm, np_, wp, need, s), norm.device,
+    _on_device(lambda s: lib.rocket_clip_grad_norm(n, p, z, c, o, oc, max_norm, np_, wp, need, s), device,
                "rocket_clip_grad_norm")
     return norm, grads if out is None else out
 

@@ -35,6 +35,7 @@ bool is_long(int P) { return parts_of(P) > kMostParts; }
 // Owners whose sums go to the workspace (a block of warps adds its own up first).
 int owners_of(int N, int P) {
     if (is_long(P)) return 0;
+    if (N <= (is_short(P) ? 64 : 2)) return 1;           // no second launch: an owner by itself writes the gradients
     const int rows = is_short(P) ? kThreads / 32 : 1;
     return std::max(1, (int)std::min<int64_t>(((int64_t)N + rows - 1) / rows, (int64_t)kSms * resident_of(P) / (is_short(P) ? 1 : parts_of(P))));
 }
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
         }
     }
     asm volatile("griddepcontrol.launch_dependents;");      // the kernel that adds up the sums waits for this one's end
-    if (!a.partial) return;
+    if (!a.dgamma && !a.dbeta) return;
     // the warps add their sums in turn
     for (int w = 0; w < kThreads / 32; ++w) {
         if ((int)(threadIdx.x >> 5) == w) {
@@ -154,6 +155,13 @@ __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
                     }
         }
         __syncthreads();
+    }
+    if (gridDim.x == 1) {
+        for (int i = threadIdx.x; i < a.P; i += kThreads) {
+            if (a.dgamma) store_typed<1>(a.dgamma, a.w_type, i, {sums[i]});
+            if (a.dbeta) store_typed<1>(a.dbeta, a.w_type, i, {sums[a.P + i]});
+        }
+        return;
     }
     float* out = a.partial + (int64_t)blockIdx.x * 2 * a.P;
     for (int i = threadIdx.x; i < 2 * a.P; i += kThreads) out[i] = sums[i];
@@ -276,7 +284,16 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
         }
     if constexpr (OWNER == kCluster) leave_cluster();
     asm volatile("griddepcontrol.launch_dependents;");
-    if (!a.partial) return;
+    if (!a.dgamma && !a.dbeta) return;
+    if (owners == 1) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (has(k)) {
+                if (a.dgamma) store_typed<W>(a.dgamma, a.w_type, beg + (first + k * step) * W, dg[k]);
+                if (a.dbeta) store_typed<W>(a.dbeta, a.w_type, beg + (first + k * step) * W, db[k]);
+            }
+        return;
+    }
     float* out = a.partial + (int64_t)owner * 2 * a.P + beg;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
@@ -467,15 +484,16 @@ cudaError_t launch_long(const Backward& a, cudaStream_t stream) {
 
 }  // namespace
 
-int64_t backward_workspace(int N, int P) { return (int64_t)owners_of(N, P) * 2 * P * (int64_t)sizeof(float); }
+int64_t backward_workspace(int N, int P) {
+    const int owners = owners_of(N, P);
+    return owners > 1 ? (int64_t)owners * 2 * P * (int64_t)sizeof(float) : 0;
+}
 
-cudaError_t launch_backward(const Backward& args, cudaStream_t stream) {
-    Backward a = args;
+cudaError_t launch_backward(const Backward& a, cudaStream_t stream) {
     if (a.N == 0 && !a.dgamma && !a.dbeta) return cudaSuccess;
-    if (!a.dgamma && !a.dbeta) a.partial = nullptr;
     auto fits = [&](int W) {
         return a.P % W == 0 && packs(a.x, a.x_type, a.N > 1 ? a.x_stride : 0, W) && packs(a.dy, a.y_type, a.N > 1 ? a.dy_stride : 0, W) &&
-               packs(a.dx, a.x_type, a.dx && a.N > 1 ? a.dx_stride : 0, W) && packs(a.gamma, a.w_type, 0, W);
+               packs(a.dx, a.x_type, a.dx && a.N > 1 ? a.dx_stride : 0, W) && packs(a.gamma, a.w_type, 0, W) && packs(a.dgamma, a.w_type, 0, W) && packs(a.dbeta, a.w_type, 0, W);
     };
     // bulk copies begin on 16-byte borders
     const bool ring = packs(a.x, ROCKET_F32, 0, 4) && packs(a.dy, ROCKET_F32, 0, 4) &&
@@ -495,7 +513,7 @@ cudaError_t launch_backward(const Backward& args, cudaStream_t stream) {
             return launch_blocks<TX, TY, 1, kColumns, false>(a, owners, stream);
         });
     });
-    if (e != cudaSuccess || is_long(a.P) || !a.partial) return e;
+    if (e != cudaSuccess || owners <= 1 || (!a.dgamma && !a.dbeta)) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((a.P + 31) / 32));
     cfg.blockDim = dim3(kSumWarps * 32);
