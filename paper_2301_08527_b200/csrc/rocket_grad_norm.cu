@@ -71,11 +71,11 @@ __device__ __forceinline__ int tensor_of(const Table<N>& t, int chunk) {
     return lo;
 }
 
-// Calls f(values, how many, position) for the words and single values of p[0 .. n) that fall to this thread, a few words at a time.
-template <int THREADS, class T, class F>
+// Calls f(values, position) for the words of W values and the single values of p[0 .. n) that fall to this thread, a few words at a time.
+template <int THREADS, class T, int W, class F>
 __device__ __forceinline__ void for_chunk(const T* p, int n, F&& f) {
-    constexpr int W = 16 / (int)sizeof(T), U = 4;
-    const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
+    constexpr int U = 64 / (W * (int)sizeof(T)), kWord = W * (int)sizeof(T);
+    const int head = min(n, (int)((kWord - (int)(reinterpret_cast<uintptr_t>(p) & (kWord - 1))) & (kWord - 1)) / (int)sizeof(T));
     const int words = (n - head) / W, tail = head + words * W;
     const T* body = p + head;
     for (int i = threadIdx.x; i < words; i += U * THREADS) {
@@ -100,7 +100,7 @@ __device__ __forceinline__ void for_chunk(const T* p, int n, F&& f) {
 
 template <int THREADS, class T>
 __device__ __forceinline__ void add_squares(const void* g, int64_t beg, int n, double (&s)[4]) {
-    for_chunk<THREADS, T>(static_cast<const T*>(g) + beg, n, [&](const auto& x, int) {
+    for_chunk<THREADS, T, 16 / (int)sizeof(T)>(static_cast<const T*>(g) + beg, n, [&](const auto& x, int) {
         constexpr int W = sizeof(x) / sizeof(float);
 #pragma unroll
         for (int j = 0; j < W; ++j) s[j & 3] = fma((double)x[j], (double)x[j], s[j & 3]);
@@ -130,7 +130,8 @@ __device__ __forceinline__ float factor(float norm, float max_norm) {
 template <int THREADS, class TG, class TO>
 __device__ __forceinline__ void scale_chunk(const void* g, void* out, int64_t beg, int n, float c) {
     TO* to = static_cast<TO*>(out) + beg;
-    for_chunk<THREADS, TG>(static_cast<const TG*>(g) + beg, n, [&](const auto& x, int at) {
+    // words of 16 bytes of the wider of the two, so that a warp's loads and stores are both of one piece
+    for_chunk<THREADS, TG, 16 / (int)(sizeof(TO) > sizeof(TG) ? sizeof(TO) : sizeof(TG))>(static_cast<const TG*>(g) + beg, n, [&](const auto& x, int at) {
         constexpr int W = sizeof(x) / sizeof(float);
         float o[W];
 #pragma unroll

@@ -306,31 +306,42 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
             }
 }
 
-// dg and db from the owners' sums: a block has 32 columns, its warps share the owners.
-constexpr int kSumWarps = 32;
-__global__ void __launch_bounds__(kSumWarps * 32) sum_owners_kernel(const float* __restrict__ partial, int owners, int P, void* dgamma, void* dbeta,
-                                                                    int w_type) {
-    __shared__ float red[2][kSumWarps][32];
+// dg and db from the owners' sums: a lane has C columns, a block 32 C, its warps share the owners.
+template <int C, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) sum_owners_kernel(const float* __restrict__ partial, int owners, int P, void* dgamma, void* dbeta, int w_type) {
+    __shared__ float red[2][WARPS][32 * C];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t p = (int64_t)blockIdx.x * 32 + lane;
+    const int64_t p = ((int64_t)blockIdx.x * 32 + lane) * C;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    float s = 0.0f, q = 0.0f;
+    float s[C] = {}, q[C] = {};
     if (p < P)
-#pragma unroll 8
-        for (int o = warp; o < owners; o += kSumWarps) {
+#pragma unroll 4
+        for (int o = warp; o < owners; o += WARPS) {
             const float* from = partial + (int64_t)o * 2 * P + p;
-            q += from[0];
-            s += from[P];
+            const Packed<float, C> a = load_packed<float, C>(from), b = load_packed<float, C>(from + P);
+            float x[C];
+            unpack<float, C>(a, x);
+#pragma unroll
+            for (int j = 0; j < C; ++j) q[j] += x[j];
+            unpack<float, C>(b, x);
+#pragma unroll
+            for (int j = 0; j < C; ++j) s[j] += x[j];
         }
-    red[0][warp][lane] = q;
-    red[1][warp][lane] = s;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        red[0][warp][lane * C + j] = q[j];
+        red[1][warp][lane * C + j] = s[j];
+    }
     __syncthreads();
-    if (warp < 2 && p < P) {
+    for (int i = threadIdx.x; i < 2 * 32 * C; i += WARPS * 32) {
+        const int which = i / (32 * C), c = i % (32 * C);
+        const int64_t column = (int64_t)blockIdx.x * 32 * C + c;
+        void* out = which == 0 ? dgamma : dbeta;
+        if (!out || column >= P) continue;
         float v[1] = {0.0f};
 #pragma unroll
-        for (int w = 0; w < kSumWarps; ++w) v[0] += red[warp][w][lane];
-        void* out = warp == 0 ? dgamma : dbeta;
-        if (out) store_typed<1>(out, w_type, p, v);
+        for (int w = 0; w < WARPS; ++w) v[0] += red[which][w][c];
+        store_typed<1>(out, w_type, column, v);
     }
 }
 
@@ -440,9 +451,11 @@ cudaError_t launch_owners(const Backward& a, int& owners, cudaStream_t stream) {
     cfg.numAttrs = OWNER == kCluster ? 1 : 0;
     if constexpr (OWNER == kCluster) {
         // not every SM finds partners in its group of SMs: clusters that would have to wait for others to end cost a second round
+        static std::atomic<uint64_t> allowed{0};
         static std::atomic<int> known[kMostParts + 1][kThreads / 32 + 1];
         int most = 0;
-        const cudaError_t e = active_clusters(known[parts][threads / 32], kernel, cfg, most);
+        cudaError_t e = parts > 8 ? once_per_device(allowed, [&] { return allow_large_clusters(kernel); }) : cudaSuccess;
+        if (e == cudaSuccess) e = active_clusters(known[parts][threads / 32], kernel, cfg, most);
         if (e != cudaSuccess) return e;
         owners = std::min(owners, most);
         cfg.gridDim = dim3((unsigned)(owners * parts));
@@ -514,17 +527,22 @@ cudaError_t launch_backward(const Backward& a, cudaStream_t stream) {
         });
     });
     if (e != cudaSuccess || owners <= 1 || (!a.dgamma && !a.dbeta)) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((a.P + 31) / 32));
-    cfg.blockDim = dim3(kSumWarps * 32);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    count_launch();
-    return cudaLaunchKernelEx(&cfg, sum_owners_kernel, (const float*)a.partial, owners, a.P, a.dgamma, a.dbeta, a.w_type);
+    auto sum = [&](auto kernel, int columns, int warps) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)((a.P + columns - 1) / columns));
+        cfg.blockDim = dim3((unsigned)(warps * 32));
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        count_launch();
+        return cudaLaunchKernelEx(&cfg, kernel, (const float*)a.partial, owners, a.P, a.dgamma, a.dbeta, a.w_type);
+    };
+    // Long rows fill the SMs with four columns a lane, and with as many warps as there are owners to share.
+    if (a.P % 4 == 0 && a.P >= 8192) return owners > 64 ? sum(sum_owners_kernel<4, 16>, 128, 16) : sum(sum_owners_kernel<4, 8>, 128, 8);
+    return sum(sum_owners_kernel<1, 32>, 32, 32);
 }
 
 }  // namespace norm

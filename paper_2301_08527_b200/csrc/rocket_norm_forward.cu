@@ -126,8 +126,8 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
         over_lane = n_lane > 0.0f ? 1.0f / n_lane : 0.0f;
     }
     const float over_block = 1.0f / (float)(words * W), over_p = 1.0f / (float)a.P;
-    // the cluster's blocks, one for every eighth lane
-    const int part_lane = threadIdx.x & 7;
+    // the cluster's blocks, a lane for each in both halves of a warp
+    const int part_lane = threadIdx.x & (kMostParts - 1);
     float n_part = 0.0f, over_part = 0.0f;
     if (OWNER == kCluster && part_lane < parts) {
         const int64_t all = a.P / W;
@@ -197,9 +197,9 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
             if constexpr (OWNER == kCluster) {
                 const float2* all = exchange.swap(make_float2(sum, square), parts, rank, turn, ok);
                 const float2 theirs = part_lane < parts ? all[part_lane] : make_float2(0.0f, 0.0f);
-                mean = add_lanes(theirs.x, 4) * over_p;
+                mean = add_lanes(theirs.x, kMostParts / 2) * over_p;
                 e = theirs.x * over_part - mean;
-                square = add_lanes(fmaf(n_part * e, e, theirs.y), 4);
+                square = add_lanes(fmaf(n_part * e, e, theirs.y), kMostParts / 2);
                 if (!ok) square = __int_as_float(0x7fc00000);
             }
         }
@@ -320,9 +320,11 @@ cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream
     cfg.numAttrs = OWNER == kCluster ? 1 : 0;
     if constexpr (OWNER == kCluster) {
         // not every SM finds partners in its group of SMs: clusters that would have to wait for others to end cost a second round
+        static std::atomic<uint64_t> allowed{0};
         static std::atomic<int> clusters[kMostParts + 1][1024 / 32 + 1];
         int at_once = 0;
-        const cudaError_t e = active_clusters(clusters[parts][threads / 32], kernel, cfg, at_once);
+        cudaError_t e = parts > 8 ? once_per_device(allowed, [&] { return allow_large_clusters(kernel); }) : cudaSuccess;
+        if (e == cudaSuccess) e = active_clusters(clusters[parts][threads / 32], kernel, cfg, at_once);
         if (e != cudaSuccess) return e;
         cfg.gridDim = dim3((unsigned)std::min<int64_t>(blocks, (int64_t)at_once * parts));
     }
@@ -351,9 +353,11 @@ cudaError_t launch_ring(const Forward& a, int threads, int parts, int resident, 
     cfg.attrs = attr;
     cfg.numAttrs = OWNER == kCluster ? 1 : 0;
     if constexpr (OWNER == kCluster) {
+        static std::atomic<uint64_t> allowed{0};
         static std::atomic<int> clusters[kMostParts + 1][1024 / 32 + 1];
         int at_once = 0;
-        e = active_clusters(clusters[parts][threads / 32], kernel, cfg, at_once);
+        if (parts > 8) e = once_per_device(allowed, [&] { return allow_large_clusters(kernel); });
+        if (e == cudaSuccess) e = active_clusters(clusters[parts][threads / 32], kernel, cfg, at_once);
         if (e != cudaSuccess) return e;
         cfg.gridDim = dim3((unsigned)(std::min(a.N, at_once) * parts));
     }

@@ -12,7 +12,7 @@ namespace rocket {
 namespace norm {
 
 constexpr int kSms = 148;
-constexpr int kMostParts = 8;             // blocks of a cluster
+constexpr int kMostParts = 16;            // blocks of a cluster
 
 enum Owner { kWarp, kBlock, kCluster };
 
@@ -83,12 +83,16 @@ inline cudaError_t once_per_device(std::atomic<uint64_t>& done, F&& set) {
     return e;
 }
 
+// Lets `kernel` run in clusters of more than eight blocks.
+template <class K>
+inline cudaError_t allow_large_clusters(K kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); }
+
 // Clusters of `kernel` that run at the same time, asked for once and kept in `known` (all devices are alike).
 template <class K>
 inline cudaError_t active_clusters(std::atomic<int>& known, K kernel, const cudaLaunchConfig_t& cfg, int& clusters) {
     clusters = known.load(std::memory_order_relaxed);
     if (clusters > 0) return cudaSuccess;
-    const cudaError_t e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+    cudaError_t e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
     clusters = std::max(clusters, 1);
     if (e == cudaSuccess) known.store(clusters, std::memory_order_relaxed);
     return e;
