@@ -5,9 +5,9 @@
 // Squares and sums are kept in double precision: fp32 gradients of 1e-20 and 1e20 both have squares outside fp32.  The sums'
 // order depends on the sizes alone.
 //
-// Bound: memory.  Two kernels: the first leaves a sum per block, every block of the second adds those up for itself and scales.  The second
-// goes through the tensors from the end, where the first has just been: what still lies in the L2 cache is not fetched again.  Tensors may
-// begin anywhere; each chunk is taken in words of 16 bytes between its first and its last such border.
+// Bound: memory.  Two kernels: the first leaves a sum per block, every block of the second adds those up for itself and scales.  Every
+// block has a contiguous share of the tensors, taken as one long line, the same in both kernels.  Tensors may begin anywhere; a
+// share's piece of one is taken in words of 16 bytes between its first and its last such border.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -27,10 +27,9 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 256;
 constexpr int kBlocks = 148 * 4;         // most blocks, and partial sums, of one launch
 constexpr int kFewTensors = 64;          // of one launch: the table travels in its arguments, of which a short one is there sooner
-constexpr int kTensors = 900;
-// Values of one tensor that a block takes at a time: few enough that a small gradient reaches every block, and at most so many that
-// finding a chunk's tensor costs nothing beside the chunk.
-constexpr int kLeastChunk = 1024, kMostChunk = 16384;
+constexpr int kTensors = 800;
+constexpr int kPiece = 1 << 24;          // values of one tensor at a time, counted in 32 bits
+constexpr int kLeast = 1024;             // values that a block is started for
 constexpr int kSmall = 128 * 1024;       // values that one cluster deals with in one launch
 constexpr int kSmallBlocks = 8, kSmallThreads = 512;
 
@@ -38,10 +37,9 @@ template <int N>
 struct Table {
     const void* g[N];
     void* out[N];
-    int64_t size[N];
-    int first[N + 1];                    // chunk with which the tensor begins
+    int64_t first[N + 1];                // values of the tensors before this one: all of them as one long line
     uint8_t g_type[N], out_type[N];
-    int tensors, chunk;
+    int tensors;
 };
 
 template <int THREADS>
@@ -59,16 +57,31 @@ __device__ __forceinline__ double block_sum(double a) {
     return a;
 }
 
-// The tensor that a chunk belongs to.
+// The tensor that a value of the line belongs to.
 template <int N>
-__device__ __forceinline__ int tensor_of(const Table<N>& t, int chunk) {
+__device__ __forceinline__ int tensor_of(const Table<N>& t, int64_t value) {
     int lo = 0, hi = t.tensors;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (t.first[mid] <= chunk) lo = mid;
+        if (t.first[mid] <= value) lo = mid;
         else hi = mid;
     }
     return lo;
+}
+
+// Calls f(tensor, position in it, how many) for the pieces of this block's share of the line, a contiguous one.  Shares begin at multiples of
+// 64 values, which keeps them on 16-byte borders where the tensors are.
+template <int N, class F>
+__device__ __forceinline__ void for_share(const Table<N>& t, int block, int blocks, F&& f) {
+    const int64_t total = t.first[t.tensors], units = (total + 63) / 64;
+    int64_t at = units * block / blocks * 64;
+    const int64_t end = min(units * (block + 1) / blocks * 64, total);
+    if (at >= end) return;
+    for (int k = tensor_of(t, at); at < end; ++k) {
+        const int64_t beg = t.first[k], stop = min(end, t.first[k + 1]);
+        for (; at < stop; at += kPiece) f(k, at - beg, (int)min((int64_t)kPiece, stop - at));
+        at = stop;
+    }
 }
 
 // Calls f(values, position) for the words of W values and the single values of p[0 .. n) that fall to this thread, a few words at a time.
@@ -99,27 +112,25 @@ __device__ __forceinline__ void for_chunk(const T* p, int n, F&& f) {
 }
 
 template <int THREADS, class T>
-__device__ __forceinline__ void add_squares(const void* g, int64_t beg, int n, double (&s)[4]) {
+__device__ __noinline__ double sum_squares(const void* g, int64_t beg, int n) {
+    double s[4] = {};
     for_chunk<THREADS, T, 16 / (int)sizeof(T)>(static_cast<const T*>(g) + beg, n, [&](const auto& x, int) {
         constexpr int W = sizeof(x) / sizeof(float);
 #pragma unroll
         for (int j = 0; j < W; ++j) s[j & 3] = fma((double)x[j], (double)x[j], s[j & 3]);
     });
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// The block's sum of squares of every blocks-th chunk.
+// Sum of squares of the block's share.
 template <int THREADS, int N>
 __device__ __forceinline__ double squares(const Table<N>& t, int block, int blocks) {
-    double s[4] = {};
-    for (int c = block; c < t.first[t.tensors]; c += blocks) {
-        const int k = tensor_of(t, c);
-        const int64_t beg = (int64_t)(c - t.first[k]) * t.chunk;
-        const int n = (int)min((int64_t)t.chunk, t.size[k] - beg);
-        if (t.g_type[k] == ROCKET_F32) add_squares<THREADS, float>(t.g[k], beg, n, s);
-        else if (t.g_type[k] == ROCKET_F16) add_squares<THREADS, __half>(t.g[k], beg, n, s);
-        else add_squares<THREADS, __nv_bfloat16>(t.g[k], beg, n, s);
-    }
-    return block_sum<THREADS>((s[0] + s[1]) + (s[2] + s[3]));
+    double s = 0.0;
+    for_share(t, block, blocks, [&](int k, int64_t beg, int n) {
+        s += t.g_type[k] == ROCKET_F32 ? sum_squares<THREADS, float>(t.g[k], beg, n)
+             : t.g_type[k] == ROCKET_F16 ? sum_squares<THREADS, __half>(t.g[k], beg, n) : sum_squares<THREADS, __nv_bfloat16>(t.g[k], beg, n);
+    });
+    return block_sum<THREADS>(s);
 }
 
 __device__ __forceinline__ float factor(float norm, float max_norm) {
@@ -127,8 +138,9 @@ __device__ __forceinline__ float factor(float norm, float max_norm) {
     return q > 1.0f ? 1.0f : q;          // a NaN stays one
 }
 
+// Not inlined, as its registers would be asked for once for every pair of types.
 template <int THREADS, class TG, class TO>
-__device__ __forceinline__ void scale_chunk(const void* g, void* out, int64_t beg, int n, float c) {
+__device__ __noinline__ void scale_chunk(const void* g, void* out, int64_t beg, int n, float c) {
     TO* to = static_cast<TO*>(out) + beg;
     // words of 16 bytes of the wider of the two, so that a warp's loads and stores are both of one piece
     for_chunk<THREADS, TG, 16 / (int)(sizeof(TO) > sizeof(TG) ? sizeof(TO) : sizeof(TG))>(static_cast<const TG*>(g) + beg, n, [&](const auto& x, int at) {
@@ -147,16 +159,12 @@ __device__ __forceinline__ void scale_chunk(const void* g, void* out, int64_t be
 
 template <int THREADS, int N>
 __device__ __forceinline__ void scale(const Table<N>& t, int block, int blocks, float c) {
-    const int chunks = t.first[t.tensors];
-    for (int i = block; i < chunks; i += blocks) {
-        const int at = chunks - 1 - i, k = tensor_of(t, at);
-        const int64_t beg = (int64_t)(at - t.first[k]) * t.chunk;
-        const int n = (int)min((int64_t)t.chunk, t.size[k] - beg);
+    for_share(t, block, blocks, [&](int k, int64_t beg, int n) {
         const bool wide = t.out_type[k] == ROCKET_F32;
         if (t.g_type[k] == ROCKET_F32) scale_chunk<THREADS, float, float>(t.g[k], t.out[k], beg, n, c);
         else if (t.g_type[k] == ROCKET_F16) wide ? scale_chunk<THREADS, __half, float>(t.g[k], t.out[k], beg, n, c) : scale_chunk<THREADS, __half, __half>(t.g[k], t.out[k], beg, n, c);
         else wide ? scale_chunk<THREADS, __nv_bfloat16, float>(t.g[k], t.out[k], beg, n, c) : scale_chunk<THREADS, __nv_bfloat16, __nv_bfloat16>(t.g[k], t.out[k], beg, n, c);
-    }
+    });
 }
 
 template <int N>
@@ -233,12 +241,12 @@ int check(int count, const void* const* grads, const int64_t* sizes, const int32
     std::vector<Span> written, read;
     if (clip) written.reserve((size_t)count);
     if (out) read.reserve((size_t)count);
-    int64_t chunks = 0;
+    int64_t total = 0;
     for (int i = 0; i < count; ++i) {
         if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40) || !is_float_type(types[i])) return ROCKET_EINVAL;
         if (out && (!is_float_type(out_types[i]) || (out_types[i] != types[i] && out_types[i] != ROCKET_F32))) return ROCKET_EINVAL;
         if (sizes[i] == 0) continue;
-        chunks += (sizes[i] + kMostChunk - 1) / kMostChunk;
+        total = std::min(total + sizes[i], int64_t(1) << 60);
         const uintptr_t g = (uintptr_t)grads[i], o = out ? (uintptr_t)out[i] : g;
         const unsigned gb = (unsigned)float_type_bytes(types[i]), ob = out ? (unsigned)float_type_bytes(out_types[i]) : gb;
         if (!g || !o || (g & (gb - 1)) || (o & (ob - 1))) return ROCKET_EINVAL;
@@ -249,7 +257,7 @@ int check(int count, const void* const* grads, const int64_t* sizes, const int32
         written.push_back(to);
         if (o != g || ob != gb) read.push_back(from);
     }
-    if (chunks > 0x7fffffff) return ROCKET_EUNSUPPORTED;
+    if (total > (int64_t(1) << 46)) return ROCKET_EUNSUPPORTED;
     // what is written overlaps nothing; what is read may overlap itself (one tensor under two names counts twice)
     sort_spans(written);
     for (size_t i = 1; i < written.size(); ++i) if (written[i].first < written[i - 1].second) return ROCKET_EINVAL;
@@ -271,27 +279,18 @@ struct Call {
     const int32_t* out_types;
 };
 
-// A power of two, the largest that gives every block of a launch a chunk.
-int chunk_of(int64_t total) {
-    int chunk = kMostChunk;
-    while (chunk > kLeastChunk && total < (int64_t)kBlocks * chunk) chunk /= 2;
-    return chunk;
-}
-
 template <int N>
-void fill(Table<N>& t, const Call& c, int beg, int end, int chunk) {
+void fill(Table<N>& t, const Call& c, int beg, int end) {
     t.tensors = 0;
-    t.chunk = chunk;
     t.first[0] = 0;
     for (int i = beg; i < end; ++i) {
         if (c.sizes[i] == 0) continue;
         const int k = t.tensors++;
         t.g[k] = c.grads[i];
         t.out[k] = c.out ? c.out[i] : const_cast<void*>(c.grads[i]);
-        t.size[k] = c.sizes[i];
         t.g_type[k] = (uint8_t)c.types[i];
         t.out_type[k] = (uint8_t)(c.out ? c.out_types[i] : c.types[i]);
-        t.first[k + 1] = t.first[k] + (int)((c.sizes[i] + chunk - 1) / chunk);
+        t.first[k + 1] = t.first[k] + c.sizes[i];
     }
 }
 
@@ -317,10 +316,10 @@ cudaError_t run(const Call& c, bool clip, float max_norm, float* norm, double* p
     int parts = 0;
     int64_t total = 0;
     for (int i = 0; i < c.count; ++i) total += c.sizes[i];
-    const int chunk = chunk_of(total);
+    auto blocks_of = [&] { return (int)std::min<int64_t>((t.first[t.tensors] + kLeast - 1) / kLeast, kBlocks); };
     if constexpr (N == kFewTensors)
         if (total <= kSmall) {
-            fill(t, c, 0, c.count, kLeastChunk);
+            fill(t, c, 0, c.count);
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(kSmallBlocks);
             cfg.blockDim = dim3(kSmallThreads);
@@ -335,8 +334,8 @@ cudaError_t run(const Call& c, bool clip, float max_norm, float* norm, double* p
             return cudaLaunchKernelEx(&cfg, small_kernel, t, norm, max_norm, clip, c.out == nullptr);
         }
     for (int beg = 0; beg < c.count; beg += N) {
-        fill(t, c, beg, std::min(c.count, beg + N), chunk);
-        const int blocks = std::min(t.first[t.tensors], kBlocks);
+        fill(t, c, beg, std::min(c.count, beg + N));
+        const int blocks = blocks_of();
         if (!blocks) continue;
         squares_kernel<N><<<blocks, kThreads, 0, stream>>>(t, part + parts);
         count_launch();
@@ -346,8 +345,8 @@ cudaError_t run(const Call& c, bool clip, float max_norm, float* norm, double* p
     }
     if (!clip || parts == 0) return launch_behind(norm_kernel, 1, stream, (const double*)part, parts, norm);
     for (int beg = (c.count - 1) / N * N; beg >= 0; beg -= N) {
-        if (c.count > N) fill(t, c, beg, std::min(c.count, beg + N), chunk);
-        const int blocks = std::min(t.first[t.tensors], kBlocks);
+        if (c.count > N) fill(t, c, beg, std::min(c.count, beg + N));
+        const int blocks = blocks_of();
         if (!blocks) continue;
         const cudaError_t e = launch_behind(scale_kernel<N>, blocks, stream, t, (const double*)part, parts, norm, max_norm, c.out == nullptr);
         if (e != cudaSuccess) return e;

@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
     // nobody waits on a barrier, or writes to another block's shared memory, before it is there
     if constexpr (OWNER == kCluster) {
         exchange.init();
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     } else {
         __syncthreads();

@@ -62,7 +62,7 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
             const int all = words, from = (int)((int64_t)all * rank / parts);
             beg = from * W;
             words = (int)((int64_t)all * (rank + 1) / parts) - from;
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
         }
         first = threadIdx.x;
         step = blockDim.x;
