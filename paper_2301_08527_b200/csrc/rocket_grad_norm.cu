@@ -84,41 +84,49 @@ __device__ __forceinline__ void for_share(const Table<N>& t, int block, int bloc
     }
 }
 
-// Calls f(values, position) for the words of W values and the single values of p[0 .. n) that fall to this thread, a few words at a time.
-template <int THREADS, class T, int W, class F>
-__device__ __forceinline__ void for_chunk(const T* p, int n, F&& f) {
-    constexpr int U = 64 / (W * (int)sizeof(T)), kWord = W * (int)sizeof(T);
-    const int head = min(n, (int)((kWord - (int)(reinterpret_cast<uintptr_t>(p) & (kWord - 1))) & (kWord - 1)) / (int)sizeof(T));
-    const int words = (n - head) / W, tail = head + words * W;
-    const T* body = p + head;
-    for (int i = threadIdx.x; i < words; i += U * THREADS) {
+// How p[0 .. n) falls into single values, words of W values on borders of a word, and single values again.
+template <class T, int W>
+struct Split {
+    int head, words;
+    __device__ __forceinline__ Split(const T* p, int n) {
+        constexpr int kWord = W * (int)sizeof(T);
+        head = min(n, (int)((kWord - (int)(reinterpret_cast<uintptr_t>(p) & (kWord - 1))) & (kWord - 1)) / (int)sizeof(T));
+        words = (n - head) / W;
+    }
+    // The single value of this thread, or n.
+    __device__ __forceinline__ int single(int n) const {
+        const int t = (int)threadIdx.x;
+        return t < head ? t : min(n, head + words * W + (t - head));
+    }
+};
+
+// Calls f(word, number) for every word of this thread; the loads of U words are under way at a time.
+template <int THREADS, int U, class T, int W, class F>
+__device__ __forceinline__ void for_words(const T* body, int words, F&& f) {
+    int i = (int)threadIdx.x;
+    for (; i + (U - 1) * THREADS < words; i += U * THREADS) {
         Packed<T, W> v[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k)
-            if (i + k * THREADS < words) v[k] = load_packed<T, W>(body + (i + k * THREADS) * W);
+        for (int k = 0; k < U; ++k) v[k] = load_packed<T, W>(body + (int64_t)(i + k * THREADS) * W);
 #pragma unroll
-        for (int k = 0; k < U; ++k)
-            if (i + k * THREADS < words) {
-                float x[W];
-                unpack<T, W>(v[k], x);
-                f(x, head + (i + k * THREADS) * W);
-            }
+        for (int k = 0; k < U; ++k) f(v[k], i + k * THREADS);
     }
-    const int single = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - head;
-    if (single < n) {
-        const float x[1] = {to_float(p[single])};
-        f(x, single);
-    }
+    for (; i < words; i += THREADS) f(load_packed<T, W>(body + (int64_t)i * W), i);
 }
 
 template <int THREADS, class T>
-__device__ __noinline__ double sum_squares(const void* g, int64_t beg, int n) {
+__device__ __noinline__ double sum_squares(const T* p, int n) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const Split<T, W> split(p, n);
     double s[4] = {};
-    for_chunk<THREADS, T, 16 / (int)sizeof(T)>(static_cast<const T*>(g) + beg, n, [&](const auto& x, int) {
-        constexpr int W = sizeof(x) / sizeof(float);
+    for_words<THREADS, 4, T, W>(p + split.head, split.words, [&](const Packed<T, W>& v, int) {
+        float x[W];
+        unpack<T, W>(v, x);
 #pragma unroll
         for (int j = 0; j < W; ++j) s[j & 3] = fma((double)x[j], (double)x[j], s[j & 3]);
     });
+    const int at = split.single(n);
+    if (at < n) s[0] = fma((double)to_float(p[at]), (double)to_float(p[at]), s[0]);
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
@@ -127,8 +135,9 @@ template <int THREADS, int N>
 __device__ __forceinline__ double squares(const Table<N>& t, int block, int blocks) {
     double s = 0.0;
     for_share(t, block, blocks, [&](int k, int64_t beg, int n) {
-        s += t.g_type[k] == ROCKET_F32 ? sum_squares<THREADS, float>(t.g[k], beg, n)
-             : t.g_type[k] == ROCKET_F16 ? sum_squares<THREADS, __half>(t.g[k], beg, n) : sum_squares<THREADS, __nv_bfloat16>(t.g[k], beg, n);
+        s += t.g_type[k] == ROCKET_F32 ? sum_squares<THREADS>(static_cast<const float*>(t.g[k]) + beg, n)
+             : t.g_type[k] == ROCKET_F16 ? sum_squares<THREADS>(static_cast<const __half*>(t.g[k]) + beg, n)
+                                         : sum_squares<THREADS>(static_cast<const __nv_bfloat16*>(t.g[k]) + beg, n);
     });
     return block_sum<THREADS>(s);
 }
@@ -138,32 +147,50 @@ __device__ __forceinline__ float factor(float norm, float max_norm) {
     return q > 1.0f ? 1.0f : q;          // a NaN stays one
 }
 
-// Not inlined, as its registers would be asked for once for every pair of types.
+// Words of 16 bytes of the wider of the two types, so that a warp's loads and stores are both of one piece.  Not inlined: the registers would
+// be asked for once for every pair of types.
 template <int THREADS, class TG, class TO>
-__device__ __noinline__ void scale_chunk(const void* g, void* out, int64_t beg, int n, float c) {
-    TO* to = static_cast<TO*>(out) + beg;
-    // words of 16 bytes of the wider of the two, so that a warp's loads and stores are both of one piece
-    for_chunk<THREADS, TG, 16 / (int)(sizeof(TO) > sizeof(TG) ? sizeof(TO) : sizeof(TG))>(static_cast<const TG*>(g) + beg, n, [&](const auto& x, int at) {
-        constexpr int W = sizeof(x) / sizeof(float);
-        float o[W];
+__device__ __noinline__ void scale_piece(const TG* g, TO* to, int n, float c) {
+    constexpr int W = 16 / (int)(sizeof(TO) > sizeof(TG) ? sizeof(TO) : sizeof(TG)), U = 64 / (W * (int)sizeof(TG));
+    const Split<TG, W> split(g, n);
+    TO* body = to + split.head;
+    auto scaled = [&](const Packed<TG, W>& v, float (&o)[W]) {
+        unpack<TG, W>(v, o);
 #pragma unroll
-        for (int j = 0; j < W; ++j) o[j] = x[j] * c;
-        if (reinterpret_cast<uintptr_t>(to + at) % Packed<TO, W>::kWord == 0) {
-            store_packed<TO, W>(to + at, o);
-        } else {
+        for (int j = 0; j < W; ++j) o[j] *= c;
+    };
+    if (reinterpret_cast<uintptr_t>(body) % Packed<TO, W>::kWord == 0) {
+        for_words<THREADS, U, TG, W>(g + split.head, split.words, [&](const Packed<TG, W>& v, int i) {
+            float o[W];
+            scaled(v, o);
+            store_packed<TO, W>(body + (int64_t)i * W, o);
+        });
+    } else {
+        for_words<THREADS, U, TG, W>(g + split.head, split.words, [&](const Packed<TG, W>& v, int i) {
+            float o[W];
+            scaled(v, o);
 #pragma unroll
-            for (int j = 0; j < W; ++j) to[at + j] = from_float<TO>(o[j]);
-        }
-    });
+            for (int j = 0; j < W; ++j) body[(int64_t)i * W + j] = from_float<TO>(o[j]);
+        });
+    }
+    const int at = split.single(n);
+    if (at < n) to[at] = from_float<TO>(to_float(g[at]) * c);
+}
+
+template <int THREADS, class TG, int N>
+__device__ __forceinline__ void scale_tensor(const Table<N>& t, int k, int64_t beg, int n, float c) {
+    const TG* g = static_cast<const TG*>(t.g[k]) + beg;
+    if constexpr (sizeof(TG) == 2)
+        if (t.out_type[k] != ROCKET_F32) return scale_piece<THREADS>(g, static_cast<TG*>(t.out[k]) + beg, n, c);
+    scale_piece<THREADS>(g, static_cast<float*>(t.out[k]) + beg, n, c);
 }
 
 template <int THREADS, int N>
 __device__ __forceinline__ void scale(const Table<N>& t, int block, int blocks, float c) {
     for_share(t, block, blocks, [&](int k, int64_t beg, int n) {
-        const bool wide = t.out_type[k] == ROCKET_F32;
-        if (t.g_type[k] == ROCKET_F32) scale_chunk<THREADS, float, float>(t.g[k], t.out[k], beg, n, c);
-        else if (t.g_type[k] == ROCKET_F16) wide ? scale_chunk<THREADS, __half, float>(t.g[k], t.out[k], beg, n, c) : scale_chunk<THREADS, __half, __half>(t.g[k], t.out[k], beg, n, c);
-        else wide ? scale_chunk<THREADS, __nv_bfloat16, float>(t.g[k], t.out[k], beg, n, c) : scale_chunk<THREADS, __nv_bfloat16, __nv_bfloat16>(t.g[k], t.out[k], beg, n, c);
+        if (t.g_type[k] == ROCKET_F32) scale_tensor<THREADS, float>(t, k, beg, n, c);
+        else if (t.g_type[k] == ROCKET_F16) scale_tensor<THREADS, __half>(t, k, beg, n, c);
+        else scale_tensor<THREADS, __nv_bfloat16>(t, k, beg, n, c);
     });
 }
 
