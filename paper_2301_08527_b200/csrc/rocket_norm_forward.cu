@@ -1,448 +1,11 @@
-// Layer norm forward: m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), y = (x - m) r g + b for every row.
-//
-// Bound: memory.  A row is read once and stays in registers while its owner's next row is on its way.  All is relative to x0, the
-// row's first value: differences of values far from zero are exact, a constant row gives 0.  A thread takes the mean c of
-// its values and the sum q of their squared distances from c; where sets of values meet, with n, c and q each, the whole has
-// c = sum n c / sum n and q = sum (q + n (c - whole's c)^2).  So the second moment is never a difference of large numbers, and the
-// threads of a block need one barrier, the blocks of a cluster one exchange per row.
-//
-// Who has a row: a warp where it is short, a block, or the blocks of a cluster where rows are few or longer than a block's
-// registers.  The owners stay and go through the rows in turn.
-#include <algorithm>
-
-#include "rocket_float_types.cuh"
-#include "rocket_internal.h"
-#include "rocket_norm.h"
-#include "rocket_norm_sums.cuh"
+// Layer norm forward: the call by the type of x.  The kernels for each are compiled in a unit of their own (rocket_norm_forward_*.cu).
+#include "rocket_norm_forward.cuh"
 
 namespace rocket {
 namespace norm {
-namespace {
-
-// Where gamma and beta come from: registers, filled once (kHold); loads of a type known at compile time, both being there (kAsFloat,
-// kAsInput: fp32, the input's); loads that ask (kAsk).
-enum Weights { kAsk, kHold, kAsFloat, kAsInput };
-
-constexpr int kMostStages = 8;
-constexpr int kSmemSm = 227 * 1024;       // shared memory of an SM
-
-// Threads that hold 32 values of x, gamma and beta each: most of a block, and of one in a cluster.
-constexpr int kHeldValues = 32, kHoldThreads = 128, kHoldClusterThreads = 160;
-
-// Blocks of an SM that the registers are cut for.
-constexpr int resident_blocks(Owner owner, Weights weights, int values) {
-    return owner == kWarp ? (values <= 10 ? 4 : values <= 14 ? 3 : 2) : weights == kHold ? (owner == kCluster ? 3 : 4) : 1;
-}
-
-// RING: a block's next rows, which lie on 16-byte borders, come into shared memory by bulk copies, as many ahead as there are stages; else
-// the threads hold the next one in registers.  A thread that gives up waiting counts as NaN, which makes the row NaN.
-// W values per word, NV words per thread.  FIT: which of a thread's words are within the row needs asking for none (2), for its
-// last (1), for all of them (0).
-// LANES: of a warp that share a row; a warp has 32 / LANES rows at a time.
-template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT, bool RING = false, int LANES = 32>
-__global__ void __launch_bounds__(OWNER == kWarp ? 256 : WEIGHTS == kHold ? (OWNER == kCluster ? kHoldClusterThreads : kHoldThreads) : 1024,
-                                  resident_blocks(OWNER, WEIGHTS, NV * W))
-rows_kernel(const Forward a, int parts, int stages, int stage_words) {
-    extern __shared__ __align__(16) unsigned char ring[];
-    __shared__ __align__(8) uint64_t arrived[RING ? kMostStages : 1];
-    int64_t row, rows;
-    int beg = 0, words = a.P / W, first, step, rank = 0;
-    __shared__ Exchange exchange;
-    if constexpr (OWNER == kWarp) {
-        row = (int64_t)blockIdx.x * (blockDim.x / LANES) + (threadIdx.x >> 5) * (32 / LANES);      // the warp's first; its lanes' below
-        rows = (int64_t)gridDim.x * (blockDim.x / LANES);
-        first = threadIdx.x & (LANES - 1);
-        step = LANES;
-    } else {
-        row = blockIdx.x / parts;
-        rows = gridDim.x / parts;
-        if constexpr (OWNER == kCluster) {
-            exchange.init();
-            rank = blockIdx.x % parts;
-            const int all = words, from = (int)((int64_t)all * rank / parts);
-            beg = from * W;
-            words = (int)((int64_t)all * (rank + 1) / parts) - from;
-            asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-        }
-        first = threadIdx.x;
-        step = blockDim.x;
-    }
-    const bool last = first + (NV - 1) * step < words;
-    auto has = [&](int k) { return FIT == 2 || (FIT == 1 ? k < NV - 1 || last : first + k * step < words); };
-    const int at = beg + first * W;
-    Packed<T, W> next[RING ? 1 : NV];
-    float next0 = 0.0f;
-    const int ahead = OWNER == kWarp ? (threadIdx.x & 31) / LANES : 0;
-    const T* source = static_cast<const T*>(a.x) + (row + ahead) * a.x_stride;
-    const int64_t source_step = rows * a.x_stride;
-    auto fetch = [&](int64_t n) {
-        const T* from = source + at;
-        if (LANES < 32 && n + ahead >= a.N) return;
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (has(k)) next[RING ? 0 : k] = load_packed_once<T, W>(from + k * step * W);
-        next0 = to_float(__ldg(source));
-        source += source_step;
-    };
-    const uint32_t bars = fast::smem_u32(arrived), rings = fast::smem_u32(ring), row_bytes = (uint32_t)(words * W * (int)sizeof(T)), stage_bytes = (uint32_t)stage_words * (W * sizeof(T));
-    int64_t to_copy = row;
-    auto copy = [&](int stage) {
-        fast::mbar_arrive_expect_tx(bars + 8u * stage, row_bytes);
-        fast::bulk_g2s(rings + (uint32_t)stage * stage_bytes, source + beg, row_bytes, bars + 8u * stage);
-        source += source_step;
-        to_copy += rows;
-    };
-    int stage = 0;
-    uint32_t parity = 0;
-    if constexpr (RING) {
-        if (threadIdx.x == 0) {
-            for (int i = 0; i < stages; ++i) fast::mbar_init(bars + 8u * i, 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-            for (int i = 0; i < stages && to_copy < a.N; ++i) copy(i);
-        }
-        if (OWNER == kCluster && row < a.N) next0 = to_float(__ldg(static_cast<const T*>(a.x) + row * a.x_stride));
-    } else {
-        if (row < a.N) fetch(row);
-    }
-    float g[WEIGHTS == kHold ? NV : 1][W], b[WEIGHTS == kHold ? NV : 1][W];
-    if constexpr (WEIGHTS == kHold)
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-#pragma unroll
-            for (int j = 0; j < W; ++j) { g[k][j] = 1.0f; b[k][j] = 0.0f; }
-            if (a.gamma && has(k)) load_typed<W>(a.gamma, a.w_type, at + k * step * W, g[k]);
-            if (a.beta && has(k)) load_typed<W>(a.beta, a.w_type, at + k * step * W, b[k]);
-        }
-    // values of this thread, its warp, its lane's warp, and the block
-    const int n_thread = ((words - first + step - 1) / step) * W;
-    const float n = (float)(words > first ? n_thread : 0), over_n = n > 0.0f ? 1.0f / n : 0.0f;
-    const float n_warp = add_lanes(n, LANES / 2), over_warp = n_warp > 0.0f ? 1.0f / n_warp : 0.0f;
-    __shared__ float warp_n[32];
-    float n_lane = 0.0f, over_lane = 0.0f;
-    if constexpr (OWNER != kWarp) {
-        if ((threadIdx.x & 31) == 0) warp_n[threadIdx.x >> 5] = n_warp;
-        __syncthreads();
-        n_lane = (threadIdx.x & 31) < (blockDim.x >> 5) ? warp_n[threadIdx.x & 31] : 0.0f;
-        over_lane = n_lane > 0.0f ? 1.0f / n_lane : 0.0f;
-    }
-    const float over_block = 1.0f / (float)(words * W), over_p = 1.0f / (float)a.P;
-    // the cluster's blocks, a lane for each in both halves of a warp
-    const int part_lane = threadIdx.x & (kMostParts - 1);
-    float n_part = 0.0f, over_part = 0.0f;
-    if (OWNER == kCluster && part_lane < parts) {
-        const int64_t all = a.P / W;
-        n_part = (float)(((int)(all * (part_lane + 1) / parts) - (int)(all * part_lane / parts)) * W);
-        over_part = 1.0f / n_part;
-    }
-    if constexpr (OWNER == kCluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    bool ok = true;
-    for (int turn = 0; row < a.N; row += rows, ++turn) {
-        float f[NV][W], x0 = next0;
-        if constexpr (RING) {
-            ok = ok && wait_soon(bars + 8u * stage, parity);
-            const T* x = reinterpret_cast<const T*>(ring + (size_t)stage * stage_bytes);
-            if constexpr (OWNER == kCluster) {
-                x0 = next0;
-                if (row + rows < a.N) next0 = to_float(__ldg(static_cast<const T*>(a.x) + (row + rows) * a.x_stride));
-            } else {
-                x0 = to_float(x[0]);
-            }
-            if (!ok) x0 = __int_as_float(0x7fc00000);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (has(k)) unpack<T, W>(load_packed<T, W>(x + (first + k * step) * W), f[k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (has(k)) unpack<T, W>(next[RING ? 0 : k], f[k]);
-            if (row + rows < a.N) fetch(row + rows);
-        }
-        float s[2] = {0.0f, 0.0f}, q[2] = {0.0f, 0.0f};         // two chains each
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (has(k))
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    f[k][j] -= x0;
-                    s[(k * W + j) & 1] += f[k][j];
-                }
-        float sum = s[0] + s[1], c = sum * over_n;
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (has(k))
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    const float d = f[k][j] - c;
-                    q[(k * W + j) & 1] = fmaf(d, d, q[(k * W + j) & 1]);
-                }
-        float square = q[0] + q[1];
-        sum = add_lanes(sum, LANES / 2);
-        float mean = sum * over_warp, e = c - mean;
-        square = add_lanes(fmaf(n * e, e, square), LANES / 2);
-        if constexpr (OWNER != kWarp) {
-            __shared__ float2 sets[2][32];                        // taken in turn: one barrier a row is enough
-            const int lane = threadIdx.x & 31;
-            if (lane == 0) sets[turn & 1][threadIdx.x >> 5] = make_float2(sum, square);
-            __syncthreads();
-            if constexpr (RING) {
-                // everybody has the row in registers: another may come into its place
-                if (threadIdx.x == 0 && ok && to_copy < a.N) copy(stage);
-                if (++stage == stages) { stage = 0; parity ^= 1u; }
-            }
-            const float2 of = lane < (int)(blockDim.x >> 5) ? sets[turn & 1][lane] : make_float2(0.0f, 0.0f);
-            sum = add_lanes(of.x, 16);
-            mean = sum * over_block;
-            e = of.x * over_lane - mean;
-            square = add_lanes(fmaf(n_lane * e, e, of.y), 16);
-            if constexpr (OWNER == kCluster) {
-                const float2* all = exchange.swap(make_float2(sum, square), parts, rank, turn, ok);
-                const float2 theirs = part_lane < parts ? all[part_lane] : make_float2(0.0f, 0.0f);
-                mean = add_lanes(theirs.x, kMostParts / 2) * over_p;
-                e = theirs.x * over_part - mean;
-                square = add_lanes(fmaf(n_part * e, e, theirs.y), kMostParts / 2);
-                if (!ok) square = __int_as_float(0x7fc00000);
-            }
-        }
-        const float r = rsqrtf(fmaf(square, over_p, a.eps)), off = -mean * r;
-        auto write = [&](auto* y) {
-            y += (row + ahead) * a.y_stride + at;
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (has(k)) {
-                    const int i = at + k * step * W, h = WEIGHTS == kHold ? k : 0;
-                    float o[W];
-                    if constexpr (WEIGHTS == kAsFloat) {
-                        unpack<float, W>(load_packed_ro<float, W>(static_cast<const float*>(a.gamma) + i), g[0]);
-                        unpack<float, W>(load_packed_ro<float, W>(static_cast<const float*>(a.beta) + i), b[0]);
-                    } else if constexpr (WEIGHTS == kAsInput) {
-                        unpack<T, W>(load_packed_ro<T, W>(static_cast<const T*>(a.gamma) + i), g[0]);
-                        unpack<T, W>(load_packed_ro<T, W>(static_cast<const T*>(a.beta) + i), b[0]);
-                    } else if constexpr (WEIGHTS == kAsk) {
-#pragma unroll
-                        for (int j = 0; j < W; ++j) { g[0][j] = 1.0f; b[0][j] = 0.0f; }
-                        if (a.gamma) load_typed<W>(a.gamma, a.w_type, i, g[0]);
-                        if (a.beta) load_typed<W>(a.beta, a.w_type, i, b[0]);
-                    }
-#pragma unroll
-                    for (int j = 0; j < W; ++j) o[j] = fmaf(fmaf(f[k][j], r, off), g[h][j], b[h][j]);
-                    store_packed(y + k * step * W, o);
-                }
-        };
-        if (LANES < 32 && row + ahead >= a.N) break;              // the warp's last turn
-        if (a.y_type == ROCKET_F32) write(static_cast<float*>(a.y));
-        else if (a.y_type == ROCKET_F16) write(static_cast<__half*>(a.y));
-        else write(static_cast<__nv_bfloat16*>(a.y));
-        if (first == 0 && rank == 0) {
-            if (a.mean) a.mean[row + ahead] = x0 + mean;
-            if (a.rstd) a.rstd[row + ahead] = r;
-        }
-    }
-    // copies that a wait gave up on must not outlive the block
-    if (RING && threadIdx.x == 0 && !ok)
-        for (int i = 0; i < stages; ++i) {
-            fast::mbar_wait(bars + 8u * stage, parity);
-            if (++stage == stages) { stage = 0; parity ^= 1u; }
-        }
-    if constexpr (OWNER == kCluster) leave_cluster();
-}
-
-// Rows longer than the registers of a cluster: a block per row, the row read three times, its sums in double precision.
-constexpr int kLongThreads = 1024;
-__device__ __forceinline__ double2 block_sums(double2 s) {
-    __shared__ double2 red[kLongThreads / 32];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        s.x += __shfl_xor_sync(0xffffffffu, s.x, o);
-        s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
-    }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
-    __syncthreads();
-    s = make_double2(0.0, 0.0);
-#pragma unroll
-    for (int w = 0; w < kLongThreads / 32; ++w) { s.x += red[w].x; s.y += red[w].y; }
-    return s;
-}
-
-template <class T>
-__global__ void __launch_bounds__(kLongThreads) long_rows_kernel(const Forward a) {
-    const T* __restrict__ x = static_cast<const T*>(a.x) + (int64_t)blockIdx.x * a.x_stride;
-    double2 s = make_double2(0.0, 0.0);
-    for (int64_t i = threadIdx.x; i < a.P; i += kLongThreads) s.x += (double)to_float(x[i]);
-    const float m = (float)(block_sums(s).x / (double)a.P);
-    s = make_double2(0.0, 0.0);
-    for (int64_t i = threadIdx.x; i < a.P; i += kLongThreads) {
-        const double d = (double)to_float(x[i]) - (double)m;
-        s.x += d;
-        s.y += d * d;
-    }
-    s = block_sums(s);
-    const double rest = s.x / (double)a.P;
-    const double v = s.y / (double)a.P - rest * rest;
-    const float r = (float)(1.0 / sqrt((v < 0.0 ? 0.0 : v) + (double)a.eps));
-    for (int64_t i = threadIdx.x; i < a.P; i += kLongThreads) {
-        float o[1] = {((to_float(x[i]) - m) - (float)rest) * r}, w[1];
-        if (a.gamma) { load_typed<1>(a.gamma, a.w_type, i, w); o[0] *= w[0]; }
-        if (a.beta) { load_typed<1>(a.beta, a.w_type, i, w); o[0] += w[0]; }
-        store_typed<1>(a.y, a.y_type, (int64_t)blockIdx.x * a.y_stride + i, o);
-    }
-    if (threadIdx.x == 0) {
-        if (a.mean) a.mean[blockIdx.x] = (float)((double)m + rest);
-        if (a.rstd) a.rstd[blockIdx.x] = r;
-    }
-}
-
-// Shared memory for a block's rows: 2 KB less than its share, for its other arrays and what the driver keeps.
-int ring_bytes(int resident) { return kSmemSm / resident - 2048; }
-
-template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT, int LANES = 32>
-cudaError_t launch(const Forward& a, int threads, int parts, cudaStream_t stream) {
-    auto kernel = rows_kernel<T, W, NV, OWNER, WEIGHTS, FIT, false, LANES>;
-    static std::atomic<int> known[1024 / 32 + 1];                        // resident blocks of an SM, by warps; all devices are alike
-    int resident = known[threads / 32].load(std::memory_order_relaxed);
-    if (resident == 0) {
-        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, 0);
-        if (e != cudaSuccess) return e;
-        known[threads / 32].store(resident, std::memory_order_relaxed);
-    }
-    const int64_t owners = OWNER == kWarp ? threads / LANES : 1;            // rows of a block
-    const int64_t most = (int64_t)kSms * std::max(resident, 1) / parts;
-    const int64_t blocks = std::min(((int64_t)a.N + owners - 1) / owners, std::max<int64_t>(most, 1)) * parts;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)parts;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = OWNER == kCluster ? 1 : 0;
-    if constexpr (OWNER == kCluster) {
-        // not every SM finds partners in its group of SMs: clusters that would have to wait for others to end cost a second round
-        static std::atomic<uint64_t> allowed{0};
-        static std::atomic<int> clusters[kMostParts + 1][1024 / 32 + 1];
-        int at_once = 0;
-        cudaError_t e = parts > 8 ? once_per_device(allowed, [&] { return allow_large_clusters(kernel); }) : cudaSuccess;
-        if (e == cudaSuccess) e = active_clusters(clusters[parts][threads / 32], kernel, cfg, at_once);
-        if (e != cudaSuccess) return e;
-        cfg.gridDim = dim3((unsigned)std::min<int64_t>(blocks, (int64_t)at_once * parts));
-    }
-    count_launch();
-    return cudaLaunchKernelEx(&cfg, kernel, a, parts, 0, 0);
-}
-
-// Blocks of `resident` per SM, each with as many stages as there is memory for.
-template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, int FIT>
-cudaError_t launch_ring(const Forward& a, int threads, int parts, int resident, cudaStream_t stream) {
-    auto kernel = rows_kernel<T, W, NV, OWNER, WEIGHTS, FIT, true>;
-    static std::atomic<uint64_t> done{0};
-    cudaError_t e = once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemSm - 4096); });
-    if (e != cudaSuccess) return e;
-    const int stage_words = (a.P / W + parts - 1) / parts, stage_bytes = stage_words * W * (int)sizeof(T);
-    const int stages = std::min(kMostStages, ring_bytes(resident) / stage_bytes);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(std::min(a.N, kSms * resident / parts) * parts));
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (size_t)stages * stage_bytes;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)parts;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = OWNER == kCluster ? 1 : 0;
-    if constexpr (OWNER == kCluster) {
-        static std::atomic<uint64_t> allowed{0};
-        static std::atomic<int> clusters[kMostParts + 1][1024 / 32 + 1];
-        int at_once = 0;
-        if (parts > 8) e = once_per_device(allowed, [&] { return allow_large_clusters(kernel); });
-        if (e == cudaSuccess) e = active_clusters(clusters[parts][threads / 32], kernel, cfg, at_once);
-        if (e != cudaSuccess) return e;
-        cfg.gridDim = dim3((unsigned)(std::min(a.N, at_once) * parts));
-    }
-    count_launch();
-    return cudaLaunchKernelEx(&cfg, kernel, a, parts, stages, stage_words);
-}
-
-template <class T, int W>
-cudaError_t launch_words(const Forward& a, cudaStream_t stream) {
-    const int words = a.P / W;
-    // Short rows: as few lanes of a warp as hold the row in up to 16 values each (up to 20 in 16 lanes, 32 in 32), since half of a warp's work
-    // would else be the sums' shuffles.
-    constexpr int kMost = W == 1 ? 16 : 32 / W, kFew = 16 / W, kMiddle = W == 1 ? 20 : 16 / W;
-    if (words <= 8 * kFew)
-        return with_int<1, kFew>((words + 7) / 8, [&](auto nv) { return launch<T, W, nv.value, kWarp, kHold, 1, 8>(a, 256, 1, stream); });
-    if (words <= 16 * kMiddle)
-        return with_int<kFew / 2 + 1, kMiddle>((words + 15) / 16, [&](auto nv) { return launch<T, W, nv.value, kWarp, kHold, 1, 16>(a, 256, 1, stream); });
-    if (words <= 32 * kMost)
-        return with_int<kMiddle / 2 + 1, kMost>((words + 31) / 32, [&](auto nv) {
-            return launch<T, W, nv.value, kWarp, nv.value * W <= 16 ? kHold : kAsk, 1>(a, 256, 1, stream);
-        });
-    constexpr int kBlockWords = W == 1 ? 16 : W == 8 ? 3 : 5;       // of a thread
-    int parts = 1;
-    while (parts < kMostParts && (words > parts * 1024 * kBlockWords || ((int64_t)parts * a.N <= kSms && a.P >= parts * 2048))) parts *= 2;
-    const int part = (words + parts - 1) / parts, least = words / parts;      // words of the blocks
-    if (part > 1024 * kBlockWords) {
-        long_rows_kernel<T><<<(unsigned)a.N, kLongThreads, 0, stream>>>(a);
-        count_launch();
-        return cudaGetLastError();
-    }
-    if constexpr (W == 1) {
-        const int nv = part <= 1024 ? 2 : part <= 4096 ? 4 : 16;
-        auto with = [&](auto n) {
-            const int threads = round32((part + n.value - 1) / n.value);
-            return parts > 1 ? launch<T, W, n.value, kCluster, kAsk, 0>(a, threads, parts, stream) : launch<T, W, n.value, kBlock, kAsk, 0>(a, threads, 1, stream);
-        };
-        return nv == 2 ? with(Int<2>()) : nv == 4 ? with(Int<4>()) : with(Int<16>());
-    } else {
-        // Enough rows: gamma and beta stay in registers, in a block where they fit, else in a cluster.
-        constexpr int kHeld = kHeldValues / W;
-        const bool bulk = a.P * (int64_t)sizeof(T) % 16 == 0 && packs(a.x, a.x_type, a.N > 1 ? a.x_stride : 0, 16 / (int)sizeof(T));
-        const int held = round32((words + kHeld - 1) / kHeld);
-        if (held <= kHoldThreads && (kHeld - 1) * held <= words && a.N > 8 * kSms) {
-            const int resident = std::min(512 / held, 8);
-            if constexpr (W * sizeof(T) == 16) if (bulk)
-                return words == kHeld * held ? launch_ring<T, W, kHeld, kBlock, kHold, 2>(a, held, 1, resident, stream)
-                                             : launch_ring<T, W, kHeld, kBlock, kHold, 1>(a, held, 1, resident, stream);
-            return launch<T, W, kHeld, kBlock, kHold, 1>(a, held, 1, stream);
-        }
-        if constexpr (W * sizeof(T) == 16) {
-            const int blocks = (words + kHeld * kHoldClusterThreads - 1) / (kHeld * kHoldClusterThreads);
-            const int most = (words + blocks - 1) / blocks, fewest = words / blocks, threads = round32((most + kHeld - 1) / kHeld);
-            if (bulk && blocks > 1 && blocks <= kMostParts && (kHeld - 1) * threads <= fewest && (int64_t)a.N * blocks >= 2 * kSms)
-                return launch_ring<T, W, kHeld, kCluster, kHold, 1>(a, threads, blocks, std::min(512 / threads, 4), stream);
-        }
-        int nv = (part + 1023) / 1024;
-        while (nv < kBlockWords && (part + nv - 1) / nv > 256 && nv * W < 16) ++nv;
-        while (nv > 1 && (nv - 1) * round32((part + nv - 1) / nv) > least) --nv;
-        return with_int<1, kBlockWords>(nv, [&](auto n) {
-            const int threads = round32((part + n.value - 1) / n.value);
-            auto with = [&](auto w) {
-                constexpr Weights WEIGHTS = decltype(w)::value;
-                return parts > 1 ? launch<T, W, n.value, kCluster, WEIGHTS, 1>(a, threads, parts, stream) : launch<T, W, n.value, kBlock, WEIGHTS, 1>(a, threads, 1, stream);
-            };
-            const bool both = a.gamma && a.beta;
-            if (both && a.w_type == ROCKET_F32) return with(std::integral_constant<Weights, kAsFloat>());
-            if constexpr (sizeof(T) == 2) if (both && a.w_type == a.x_type) return with(std::integral_constant<Weights, kAsInput>());
-            return with(std::integral_constant<Weights, kAsk>());
-        });
-    }
-}
-
-}  // namespace
 
 cudaError_t launch_forward(const Forward& a, cudaStream_t stream) {
-    return with_float_type(a.x_type, [&](auto* tx) {
-        using T = std::remove_pointer_t<decltype(tx)>;
-        auto fits = [&](int W) {
-            return a.P % W == 0 && packs(a.x, a.x_type, a.N > 1 ? a.x_stride : 0, W) && packs(a.y, a.y_type, a.N > 1 ? a.y_stride : 0, W) &&
-                   packs(a.gamma, a.w_type, 0, W) && packs(a.beta, a.w_type, 0, W);
-        };
-        if constexpr (sizeof(T) == 2) if (a.y_type != ROCKET_F32 && fits(8)) return launch_words<T, 8>(a, stream);
-        if (fits(4)) return launch_words<T, 4>(a, stream);
-        return launch_words<T, 1>(a, stream);
-    });
+    return with_float_type(a.x_type, [&](auto* tx) { return launch_rows<std::remove_pointer_t<decltype(tx)>>(a, stream); });
 }
 
 }  // namespace norm

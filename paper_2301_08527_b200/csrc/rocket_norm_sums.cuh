@@ -16,12 +16,56 @@ constexpr int kMostParts = 16;            // blocks of a cluster
 
 enum Owner { kWarp, kBlock, kCluster };
 
+// How the words of a block's threads lie in its part of a row.  kFull: all threads have all their words.  kLast: all but the last for all.  Both with rows
+// that bulk copies bring whole.  kEnd: as kLast, but a row may begin and end anywhere.  kAny: so, and threads may have fewer words.  Where a row comes
+// from shared memory, a word beyond the end is then read as the last one, which keeps the loads of all words under way at once, and counts as
+// nothing.
+enum Fit { kAny, kEnd, kLast, kFull };
+
 // A bounded wait that does not sleep at first: what it waits for is nearly always there, or about to be.
 __device__ __forceinline__ bool wait_soon(uint32_t bar, uint32_t parity) {
     for (int i = 0; i < 8; ++i)
         if (fast::mbar_try(bar, parity)) return true;
     return fast::mbar_wait(bar, parity);
 }
+
+// Bytes of shared memory for a part of a row that may begin anywhere between two 16-byte borders.
+__host__ __device__ constexpr int room_of(int part, int bytes) { return (part * bytes + 16 + 127) / 128 * 128; }
+
+// A piece of a row, n values at p, on its way to shared memory.  Bulk copies bring the whole 16-byte units within it, to the same place relative to
+// a 16-byte border; the up to 7 values before the first and behind the last border are stored there by a lane each.
+template <class T>
+struct Piece {
+    int skew, head, tail;         // bytes from the last border to p; values before the first copied one; the first value behind the copied ones
+    __device__ __forceinline__ Piece(const T* p, int n) {
+        skew = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+        head = ((16 - skew) & 15) / (int)sizeof(T);
+        tail = max(head, (int)(((unsigned)skew + (unsigned)n * (unsigned)sizeof(T)) / 16u * 16u - (unsigned)skew) / (int)sizeof(T));
+    }
+    __device__ __forceinline__ uint32_t copied() const { return (uint32_t)((tail - head) * (int)sizeof(T)); }
+    __device__ __forceinline__ void copy(uint32_t dst, const T* p, uint32_t bar) const {
+        if (tail > head) fast::bulk_g2s(dst + (uint32_t)(skew + head * (int)sizeof(T)), p + head, copied(), bar);
+    }
+};
+
+// What one of 16 lanes has to bring of a piece: where to put it (bytes from the piece's place in shared memory; -1: nothing) and its bits.
+template <class T>
+struct Edge {
+    int to = -1;
+    std::conditional_t<sizeof(T) == 4, unsigned, unsigned short> bits = 0;
+    __device__ __forceinline__ void fetch(const T* p, int n, int lane) {
+        const Piece<T> piece(p, n);
+        const int i = lane < 8 ? lane : piece.tail + lane - 8;
+        to = -1;
+        if (lane < 8 ? i < piece.head && i < n : i < n) {
+            to = piece.skew + i * (int)sizeof(T);
+            bits = __ldg(reinterpret_cast<const decltype(bits)*>(p + i));
+        }
+    }
+    __device__ __forceinline__ void put(unsigned char* place) const {
+        if (to >= 0) *reinterpret_cast<std::remove_const_t<decltype(bits)>*>(place + to) = bits;
+    }
+};
 
 // Sums over the lanes whose numbers differ in the bits from `from` down, the same bits in each.
 __device__ __forceinline__ float add_lanes(float v, int from) {
