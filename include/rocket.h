@@ -315,14 +315,15 @@ int rocket_layer_norm_backward(const void* dy_dev, int y_type, int64_t dy_stride
  *   norm_dev   [1] fp32, written: the norm before clipping
  *   out_dev, out_types  HOST arrays of the tensors that receive the clipped gradient, each of its gradient's type or fp32;
  *              out_dev NULL: in place.  An entry may be its own gradient (of the same type)
- *   workspace_dev  workspace_bytes >= rocket_grad_norm_workspace(count)
+ *   workspace_dev  workspace_bytes >= rocket_grad_norm_workspace(count, sizes) (ROCKET_EINVAL for sizes out of range); NULL is
+ *              allowed where that is 0, as it is for a small gradient in few tensors
  * Squares and sums are taken in double precision: no finite gradient overflows or vanishes in them.  The same call gives the
  * same bits each time.  An infinite norm gives c = 0 (for max_norm finite), a NaN gives NaN everywhere; a caller that would
  * rather skip such a step reads norm_dev.  ROCKET_EINVAL for a NULL or misaligned pointer, a negative count or size, an unknown or
  * unfitting type, max_norm negative or NaN, and where anything written overlaps anything else (one tensor listed twice can be
  * measured, not clipped).
  */
-int64_t rocket_grad_norm_workspace(int count);
+int64_t rocket_grad_norm_workspace(int count, const int64_t* sizes);
 int rocket_grad_norm(int count, const void* const* grads_dev, const int64_t* sizes, const int32_t* types, float* norm_dev,
                      void* workspace_dev, int64_t workspace_bytes, void* cuda_stream);
 int rocket_clip_grad_norm(int count, const void* const* grads_dev, const int64_t* sizes, const int32_t* types,

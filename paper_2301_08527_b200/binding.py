@@ -83,7 +83,7 @@ SIGNATURES = {
                                                   ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
                                                   ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
                                                   ctypes.c_void_p]),
-    "rocket_grad_norm_workspace": (ctypes.c_int64, [ctypes.c_int]),
+    "rocket_grad_norm_workspace": (ctypes.c_int64, [ctypes.c_int, ctypes.c_void_p]),
     "rocket_grad_norm": (ctypes.c_int, [ctypes.c_int] + [ctypes.c_void_p] * 5 + [ctypes.c_int64, ctypes.c_void_p]),
     "rocket_clip_grad_norm": (ctypes.c_int, [ctypes.c_int] + [ctypes.c_void_p] * 5 + [ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p,
                                                                                       ctypes.c_int64, ctypes.c_void_p]),
@@ -439,11 +439,11 @@ def _types():
 
 
 def _on_device(call, device, where):
-    """Runs call(stream) with `device` current, on that device's current stream."""
-    if device.index == _current_device():
+    """Runs call(stream) with the device of that number current, on its current stream."""
+    if device == _current_device():
         status = call(_current_stream())
     else:
-        with _torch.cuda.device(device.index):
+        with _torch.cuda.device(device):
             status = call(_current_stream())
     if status:
         raise RocketError(status, where)
@@ -453,7 +453,8 @@ def _rows(t, name, shape=None, device=None, dtype=None):
     """(pointer, type code, row stride, N, P) of a CUDA tensor taken as rows of its last dimension: two dimensions with
     any distance between the rows, or any number of contiguous ones."""
     try:
-        code = _types().get(t.dtype)
+        kind = t.dtype
+        code = _types().get(kind)
         if code is None or not t.is_cuda:
             raise AttributeError
     except AttributeError:
@@ -462,9 +463,9 @@ def _rows(t, name, shape=None, device=None, dtype=None):
     if shape is not None:
         if got != shape:
             raise ValueError("%s must have the shape %s" % (name, tuple(shape)))
-        if t.device != device:
+        if t.get_device() != device:
             raise ValueError("%s is on another device" % name)
-        if dtype is not None and t.dtype is not dtype:
+        if dtype is not None and kind is not dtype:
             raise TypeError("%s must be of dtype %s" % (name, dtype))
     if len(got) == 2:
         N, P = got
@@ -491,17 +492,16 @@ def _like(t, dtype):
 
 
 def _vector(t, n, name, device, dtype=None):
-    """(pointer, type code) of a contiguous CUDA tensor of n values, (None, None) of None."""
-    if t is None:
-        return None, None
+    """(pointer, type code) of a contiguous tensor of n values on that device."""
     try:
-        code = _types().get(t.dtype)
-        if code is None or not t.is_cuda or not t.is_contiguous() or (dtype is not None and t.dtype is not dtype):
-            raise TypeError("%s must be a contiguous CUDA tensor of dtype %s" % (name, dtype or "float32, float16 or bfloat16"))
+        kind = t.dtype
+        code = _types().get(kind)
+        if code is None or not t.is_cuda or not t.is_contiguous() or (dtype is not None and kind is not dtype):
+            raise AttributeError
     except AttributeError:
-        raise TypeError("%s must be a tensor" % name) from None
-    if t.numel() != n or t.device != device:
-        raise ValueError("%s must hold %d values on the device of the rows" % (name, n))
+        raise TypeError("%s must be a contiguous CUDA tensor of dtype %s" % (name, dtype or "float32, float16 or bfloat16")) from None
+    if t.numel() != n or t.get_device() != device:
+        raise ValueError("%s must hold %d values on the device of the other tensors" % (name, n))
     return t.data_ptr(), code
 
 
@@ -511,7 +511,7 @@ def rocket_layer_norm(feat, gamma=None, beta=None, eps=1e-5, out=None, out_dtype
     type, or None.  Returns (out, mean, rstd), the statistics fp32, one per row, or None without want_stats."""
     torch = _t()
     x, xt, xs, N, P = _rows(feat, "feat")
-    device, y = feat.device, out
+    device, y = feat.get_device(), out
     if y is not None:
         yp, yt, ys, _, _ = _rows(y, "out", feat.shape, device, out_dtype)
     else:
@@ -532,7 +532,7 @@ def rocket_layer_norm(feat, gamma=None, beta=None, eps=1e-5, out=None, out_dtype
     if mean is not None:
         mp = _vector(mean, N, "mean_out", device, torch.float32)[0]
     elif want_stats:
-        mean = torch.empty(N if feat.dim() == 2 else feat.shape[:-1], dtype=torch.float32, device=device)
+        mean = torch.empty(N if feat.dim() == 2 else feat.shape[:-1], dtype=torch.float32, device=feat.device)
         mp = mean.data_ptr()
     if rstd is not None:
         rp = _vector(rstd, N, "rstd_out", device, torch.float32)[0]
@@ -551,12 +551,10 @@ def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dg
     torch = _t()
     f32 = torch.float32
     x, xt, xs, N, P = _rows(feat, "feat")
-    device = feat.device
+    device, place = feat.get_device(), feat.device
     d, yt, ds, _, _ = _rows(dy, "dy", feat.shape, device)
     mp = _vector(mean, N, "mean", device, f32)[0]
     rp = _vector(rstd, N, "rstd", device, f32)[0]
-    if mp is None or rp is None:
-        raise TypeError("mean and rstd must be the statistics of the forward pass")
     g = wt = None
     if gamma is not None:
         g, wt = _vector(gamma, P, "gamma", device)
@@ -580,19 +578,19 @@ def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dg
     if dg is not None:
         dgp = _vector(dg, P, "dgamma_out", device, weight_dtype)[0]
     elif want_weights:
-        dg = torch.empty(P, dtype=weight_dtype, device=device)
+        dg = torch.empty(P, dtype=weight_dtype, device=place)
         dgp = dg.data_ptr()
     if db is not None:
         dbp = _vector(db, P, "dbeta_out", device, weight_dtype)[0]
     elif want_weights:
-        db = torch.empty(P, dtype=weight_dtype, device=device)
+        db = torch.empty(P, dtype=weight_dtype, device=place)
         dbp = db.data_ptr()
     lib = _lib or load_library()
     need, wp = 0, None
     if dgp or dbp:
         need = lib.rocket_layer_norm_backward_workspace(N, P)
         if need > 0:
-            ws = torch.empty(need // 4, dtype=f32, device=device)
+            ws = torch.empty(need // 4, dtype=f32, device=place)
             wp = ws.data_ptr()
     fn = lib.rocket_layer_norm_backward
     _on_device(lambda s: fn(d, yt, ds, x, xt, xs, N, P, g, wt, mp, rp, dxp, dxs, dgp, dbp, wp, need, s), device,
@@ -614,7 +612,7 @@ def _dense(t):
 
 
 def _tensor_list(ts, name):
-    """(count, addresses, sizes, type codes, device, all contiguous) of a sequence of CUDA tensors, as arrays.  Long lists are the
+    """(count, addresses, sizes, type codes, device number, all contiguous) of a sequence of CUDA tensors, as arrays.  Long lists are the
     rule, so every property is asked for in one sweep."""
     Tensor = _t().Tensor
     types = _types()
@@ -634,34 +632,34 @@ def _tensor_list(ts, name):
         raise TypeError("%s must be dense CUDA tensors of float32, float16 or bfloat16" % name) from None
     if len(devices) != 1:
         raise ValueError("%s must be on one device" % name)
-    return len(ts), ptrs, sizes, array.array("i", codes), ts[0].device, contiguous
+    return len(ts), ptrs, sizes, array.array("i", codes), devices.pop(), contiguous
 
 
 def _address(a):
     return None if a is None else a.buffer_info()[0]
 
 
-def _norm_buffers(lib, count, grads, norm_out):
+def _norm_buffers(lib, count, sizes, grads, norm_out):
     torch = _torch
     f32 = torch.float32
-    device = grads[0].device if count else norm_out.device if norm_out is not None else torch.device("cuda", _current_device())
+    place = grads[0].device if count else norm_out.device if norm_out is not None else torch.device("cuda", _current_device())
     if norm_out is not None:
-        norm, np_ = norm_out, _vector(norm_out, 1, "norm_out", device, f32)[0]
+        norm, np_ = norm_out, _vector(norm_out, 1, "norm_out", place.index, f32)[0]
     else:
-        norm = torch.empty(1, dtype=f32, device=device)
+        norm = torch.empty(1, dtype=f32, device=place)
         np_ = norm.data_ptr()
-    need = lib.rocket_grad_norm_workspace(count)
-    ws = torch.empty(need // 4, dtype=f32, device=device)
-    return ws, ws.data_ptr(), need, norm, np_, device
+    need = lib.rocket_grad_norm_workspace(count, sizes)
+    ws = torch.empty(need // 4, dtype=f32, device=place) if need > 0 else None
+    return ws, ws.data_ptr() if need > 0 else None, need, norm, np_, place.index
 
 
 def rocket_grad_norm(grads, norm_out=None):
     """2-norm of a gradient held in many tensors (a list or tuple of dense CUDA tensors of float32, float16 or bfloat16 on one
     device).  Returns it as a [1] float32 tensor."""
-    lib = _lib or load_library()
     n, ptrs, sizes, codes, _, _ = _tensor_list(grads, "grads")
-    ws, wp, need, norm, np_, device = _norm_buffers(lib, n, grads, norm_out)
+    lib = _lib or load_library()
     p, z, c = _address(ptrs), _address(sizes), _address(codes)
+    ws, wp, need, norm, np_, device = _norm_buffers(lib, n, z, grads, norm_out)
     _on_device(lambda s: lib.rocket_grad_norm(n, p, z, c, np_, wp, need, s), device, "rocket_grad_norm")
     return norm
 
@@ -680,8 +678,8 @@ def rocket_clip_grad_norm(grads, max_norm, out=None, norm_out=None):
         if not (contiguous and out_contiguous) and any(
                 a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
             raise ValueError("out must have the shapes and strides of the gradients")
-    ws, wp, need, norm, np_, device = _norm_buffers(lib, n, grads, norm_out)
     p, z, c, o, oc = _address(ptrs), _address(sizes), _address(codes), _address(outs), _address(out_codes)
+    ws, wp, need, norm, np_, device = _norm_buffers(lib, n, z, grads, norm_out)
     _on_device(lambda s: lib.rocket_clip_grad_norm(n, p, z, c, o, oc, max_norm, np_, wp, need, s), device,
                "rocket_clip_grad_norm")
     return norm, grads if out is None else out

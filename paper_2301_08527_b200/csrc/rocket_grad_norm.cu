@@ -254,26 +254,42 @@ void sort_spans(std::vector<Span>& s) {
     if (!std::is_sorted(s.begin(), s.end())) std::sort(s.begin(), s.end());
 }
 
-int64_t workspace_bytes_for(int count) { return (int64_t)sizeof(double) * kBlocks * std::max<int64_t>(1, (count + (int64_t)kTensors - 1) / kTensors); }
+// Whether one cluster deals with all of it, in one launch and without a workspace.
+bool is_small(int count, int64_t total) { return count <= kFewTensors && total <= kSmall; }
+
+// Of valid sizes.
+int64_t workspace_bytes_for(int count, int64_t total) {
+    return is_small(count, total) ? 0 : (int64_t)sizeof(double) * kBlocks * std::max<int64_t>(1, (count + (int64_t)kTensors - 1) / kTensors);
+}
+
+// All values, or -1 for a size out of range.
+int64_t total_of(int count, const int64_t* sizes) {
+    int64_t total = 0;
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40)) return -1;
+        total = std::min(total + sizes[i], int64_t(1) << 60);
+    }
+    return total;
+}
 
 // The arguments of both entry points; clip: whether gradients are written, to `out` or, where it is NULL, in place.
 int check(int count, const void* const* grads, const int64_t* sizes, const int32_t* types, bool clip, void* const* out, const int32_t* out_types,
           const float* norm, const void* workspace, int64_t workspace_bytes) {
     if (count < 0 || !norm || (reinterpret_cast<uintptr_t>(norm) & 3u)) return ROCKET_EINVAL;
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u) || workspace_bytes < workspace_bytes_for(count)) return ROCKET_EINVAL;
     if (count > 0 && (!grads || !sizes || !types || (out && !out_types))) return ROCKET_EINVAL;
-    const Span own[] = {{(uintptr_t)norm, (uintptr_t)norm + 4}, {(uintptr_t)workspace, (uintptr_t)workspace + (uintptr_t)workspace_bytes_for(count)}};
+    const int64_t total = total_of(count, sizes), need = workspace_bytes_for(count, total);
+    if (total < 0 || workspace_bytes < need || (need > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u)))) return ROCKET_EINVAL;
+    const uintptr_t ws = need > 0 ? (uintptr_t)workspace : 0;
+    const Span own[] = {{(uintptr_t)norm, (uintptr_t)norm + 4}, {ws, ws + (uintptr_t)need}};
     auto meets = [](const Span& a, const Span& b) { return a.first < b.second && b.first < a.second; };
     if (meets(own[0], own[1])) return ROCKET_EINVAL;
     std::vector<Span> written, read;
     if (clip) written.reserve((size_t)count);
     if (out) read.reserve((size_t)count);
-    int64_t total = 0;
     for (int i = 0; i < count; ++i) {
-        if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40) || !is_float_type(types[i])) return ROCKET_EINVAL;
+        if (!is_float_type(types[i])) return ROCKET_EINVAL;
         if (out && (!is_float_type(out_types[i]) || (out_types[i] != types[i] && out_types[i] != ROCKET_F32))) return ROCKET_EINVAL;
         if (sizes[i] == 0) continue;
-        total = std::min(total + sizes[i], int64_t(1) << 60);
         const uintptr_t g = (uintptr_t)grads[i], o = out ? (uintptr_t)out[i] : g;
         const unsigned gb = (unsigned)float_type_bytes(types[i]), ob = out ? (unsigned)float_type_bytes(out_types[i]) : gb;
         if (!g || !o || (g & (gb - 1)) || (o & (ob - 1))) return ROCKET_EINVAL;
@@ -341,11 +357,9 @@ template <int N>
 cudaError_t run(const Call& c, bool clip, float max_norm, float* norm, double* part, cudaStream_t stream) {
     Table<N> t;
     int parts = 0;
-    int64_t total = 0;
-    for (int i = 0; i < c.count; ++i) total += c.sizes[i];
     auto blocks_of = [&] { return (int)std::min<int64_t>((t.first[t.tensors] + kLeast - 1) / kLeast, kBlocks); };
     if constexpr (N == kFewTensors)
-        if (total <= kSmall) {
+        if (is_small(c.count, total_of(c.count, c.sizes))) {
             fill(t, c, 0, c.count);
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(kSmallBlocks);
@@ -398,7 +412,11 @@ int call(const Call& c, bool clip, float max_norm, float* norm, void* workspace,
 
 using namespace rocket;
 
-extern "C" int64_t rocket_grad_norm_workspace(int count) { return count < 0 ? ROCKET_EINVAL : workspace_bytes_for(count); }
+extern "C" int64_t rocket_grad_norm_workspace(int count, const int64_t* sizes) {
+    if (count < 0 || (count > 0 && !sizes)) return ROCKET_EINVAL;
+    const int64_t total = total_of(count, sizes);
+    return total < 0 ? ROCKET_EINVAL : workspace_bytes_for(count, total);
+}
 
 extern "C" int rocket_grad_norm(int count, const void* const* grads_dev, const int64_t* sizes, const int32_t* types, float* norm_dev,
                                 void* workspace_dev, int64_t workspace_bytes, void* cuda_stream) {

@@ -25,7 +25,17 @@ constexpr int kWarpColumns = 32 * kColumns;
 constexpr int kSmemSm = 227 * 1024;       // shared memory of an SM
 
 inline bool is_short(int P) { return P <= kWarpColumns; }
-inline int parts_of(int P) { return (P + kThreads * kColumns - 1) / (kThreads * kColumns); }
+// Blocks of a row: one or two more than the columns ask for where that gives all threads all words but the last (narrow words, of an odd P, are the harder to
+// divide).
+inline int parts_of(int P) {
+    const int fewest = (P + kThreads * kColumns - 1) / (kThreads * kColumns);
+    if (fewest == 1) return 1;
+    for (int parts = fewest; parts < fewest + 3; ++parts) {
+        const int part = ((P + parts - 1) / parts + 7) / 8 * 8, threads = round32((part + kColumns - 1) / kColumns);
+        if (P - (parts - 1) * part >= (P % 4 ? kColumns - 1 : kColumns - 4) * threads) return parts;
+    }
+    return fewest;
+}
 // Columns of a block: a multiple of 8, which keeps every part of a row on a 16-byte border.
 inline int part_of(int P) { const int parts = parts_of(P); return ((P + parts - 1) / parts + 7) / 8 * 8; }
 inline int threads_of(int P) { return round32((part_of(P) + kColumns - 1) / kColumns); }

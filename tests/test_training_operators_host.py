@@ -72,8 +72,14 @@ def test_backward_refuses_a_workspace_that_is_too_small(lib, N, P):
 def test_workspace_sizes_out_of_range(lib):
     assert lib.rocket_layer_norm_backward_workspace(-1, 10) == EINVAL
     assert lib.rocket_layer_norm_backward_workspace(10, 0) == EINVAL
-    assert lib.rocket_grad_norm_workspace(-1) == EINVAL
-    assert lib.rocket_grad_norm_workspace(0) > 0
+    sizes = (ctypes.c_int64 * 2)(1 << 30, 5)
+    assert lib.rocket_grad_norm_workspace(-1, sizes) == EINVAL
+    assert lib.rocket_grad_norm_workspace(1, None) == EINVAL
+    assert lib.rocket_grad_norm_workspace(2, (ctypes.c_int64 * 2)(5, -1)) == EINVAL
+    assert lib.rocket_grad_norm_workspace(1, (ctypes.c_int64 * 1)(1 << 60)) == EINVAL
+    assert lib.rocket_grad_norm_workspace(0, None) == 0
+    assert lib.rocket_grad_norm_workspace(2, (ctypes.c_int64 * 2)(100, 0)) == 0
+    assert lib.rocket_grad_norm_workspace(2, sizes) > 0
 
 
 def test_no_rows_are_a_no_op(lib):
@@ -83,7 +89,7 @@ def test_no_rows_are_a_no_op(lib):
 def _grads(lib, tensors, out=None, max_norm=1.0, norm=E, ws=0x7f0000000000, nbytes=None, clip=True, count=None, null=()):
     """tensors, out: lists of (address, size, type)."""
     n = len(tensors) if count is None else count
-    nbytes = lib.rocket_grad_norm_workspace(max(n, 0)) if nbytes is None else nbytes
+    nbytes = 1 << 20 if nbytes is None else nbytes
     ptr = lambda ts: (ctypes.c_void_p * len(ts))(*[t[0] for t in ts])  # noqa: E731
     sizes = (ctypes.c_int64 * len(tensors))(*[t[1] for t in tensors])
     codes = lambda ts: (ctypes.c_int32 * len(ts))(*[t[2] for t in ts])  # noqa: E731
@@ -96,13 +102,14 @@ def _grads(lib, tensors, out=None, max_norm=1.0, norm=E, ws=0x7f0000000000, nbyt
 
 
 ONE = [(A, 100, F32), (B, 7, F16)]
+LARGE = [(A, 1 << 20, F32), (B, 7, F16)]
 
 
 @pytest.mark.parametrize("clip", [False, True])
 @pytest.mark.parametrize("kw", [
-    dict(norm=None), dict(norm=E + 2), dict(ws=None), dict(ws=0x7f0000000008), dict(nbytes=15), dict(count=-1), dict(null=(0,)), dict(null=(1,)), dict(null=(2,)),
+    dict(norm=None), dict(norm=E + 2), dict(tensors=LARGE, ws=None), dict(tensors=LARGE, ws=0x7f0000000008), dict(tensors=LARGE, nbytes=15), dict(nbytes=-1), dict(count=-1), dict(null=(0,)), dict(null=(1,)), dict(null=(2,)),
     dict(tensors=[(A, -1, F32)]), dict(tensors=[(A, 1, 3)]), dict(tensors=[(A, 1, -1)]), dict(tensors=[(None, 1, F32)]), dict(tensors=[(A + 2, 1, F32)]),
-    dict(tensors=[(A + 1, 1, BF16)]), dict(tensors=[(A, 1 << 60, F32)]), dict(norm=A + 4), dict(ws=A), dict(ws=E - 64),
+    dict(tensors=[(A + 1, 1, BF16)]), dict(tensors=[(A, 1 << 60, F32)]), dict(norm=A + 4), dict(tensors=LARGE, ws=A), dict(tensors=LARGE, ws=E - 64),
 ])
 def test_norms_refuse(lib, clip, kw):
     kw = dict(kw)
