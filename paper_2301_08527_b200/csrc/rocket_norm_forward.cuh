@@ -1,10 +1,11 @@
 // Layer norm forward: m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), y = (x - m) r g + b for every row.
 //
-// Bound: memory.  A row is read once and stays in registers while its owner's next row is on its way.  All is relative to x0, the
-// row's first value: differences of values far from zero are exact, a constant row gives 0.  A thread takes the mean c of
-// its values and the sum q of their squared distances from c; where sets of values meet, with n, c and q each, the whole has
-// c = sum n c / sum n and q = sum (q + n (c - whole's c)^2).  So the second moment is never a difference of large numbers, and the
-// threads of a block need one barrier, the blocks of a cluster one exchange per row.
+// Bound: memory.  A row is read once and stays in registers while its owner's next row is on its way.  All is relative to a base: the row's
+// first value where the first three lie close together beside their distance from zero, as in a row far from zero or a constant one, whose
+// differences are then exact, else 0, which leaves small means exact.  A thread takes the mean c of its values and the sum q of their squared
+// distances from c; where sets of values meet, with n, c and q each, the whole has c = sum n c / sum n and q = sum (q + n (c - whole's c)^2).
+// So the second moment is never a difference of large numbers, and the threads of a block need one barrier, the blocks of a cluster one exchange
+// per row.
 //
 // Who has a row: a warp where it is short, a block, or the blocks of a cluster where rows are few or longer than a block's
 // registers.  The owners stay and go through the rows in turn.
@@ -30,6 +31,11 @@ constexpr int kSmemSm = 227 * 1024;       // shared memory of an SM
 // Threads that hold gamma and beta: 32 values of each, or 16 where they are loaded one by one; most threads of a block, and of one in a cluster.
 constexpr int held_values(int W) { return W == 1 ? 16 : 32; }
 constexpr int hold_threads(Owner owner, int values) { return values < 16 ? 1024 : (owner == kCluster ? 160 : 128) * (32 / values); }
+
+__device__ __forceinline__ float base_of(float a, float b, float c) {
+    const float near = 0.25f * fabsf(a);
+    return fabsf(b - a) <= near && fabsf(c - a) <= near ? a : 0.0f;
+}
 
 // Blocks of an SM that the registers are cut for.
 constexpr int resident_blocks(Owner owner, Weights weights, int values) {
@@ -71,10 +77,16 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
     const bool last = first + (NV - 1) * step < words;
     auto has = [&](int k) { return FIT == kFull || (FIT == kAny ? first + k * step < words : k < NV - 1 || last); };
     constexpr bool kEdges = RING && (FIT == kAny || FIT == kEnd);
-    auto may_miss = [](int k) { return kEdges && (FIT == kAny || k == NV - 1); };      // read all the same, as x0
+    auto may_miss = [](int k) { return kEdges && (FIT == kAny || k == NV - 1); };      // read all the same, as the base
     const int at = beg + first * W;
     Packed<T, W> next[RING ? 1 : NV];
-    float next0 = 0.0f;
+    T next_head[3] = {};                                   // the next row's first values
+    const int second = min(1, a.P - 1), third = min(2, a.P - 1);
+    auto fetch_head = [&](const T* x) {
+        next_head[0] = __ldg(x);
+        next_head[1] = __ldg(x + second);
+        next_head[2] = __ldg(x + third);
+    };
     const int ahead = OWNER == kWarp ? (threadIdx.x & 31) / LANES : 0;
     const T* source = static_cast<const T*>(a.x) + (row + ahead) * a.x_stride;
     const int64_t source_step = rows * a.x_stride;
@@ -84,7 +96,7 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (has(k)) next[RING ? 0 : k] = load_packed_once<T, W>(from + k * step * W);
-        next0 = to_float(__ldg(source));
+        fetch_head(source);
         source += source_step;
     };
     const uint32_t bars = fast::smem_u32(arrived), rings = fast::smem_u32(ring), stage_bytes = (uint32_t)room_of(stage_words * W, sizeof(T));
@@ -122,7 +134,7 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
             edge.put(ring);
             fetch_edge(row + rows);
         }
-        if ((OWNER == kCluster || kEdges) && row < a.N) next0 = to_float(__ldg(static_cast<const T*>(a.x) + row * a.x_stride));
+        if ((OWNER == kCluster || kEdges) && row < a.N) fetch_head(static_cast<const T*>(a.x) + row * a.x_stride);
     } else {
         if (row < a.N) fetch(row);
     }
@@ -159,7 +171,7 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
     if constexpr (OWNER == kCluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     bool ok = true;
     for (int turn = 0; row < a.N; row += rows, ++turn) {
-        float f[NV][W], x0 = next0;
+        float f[NV][W], base = base_of(to_float(next_head[0]), to_float(next_head[1]), to_float(next_head[2]));
         if constexpr (RING) {
             ok = ok && wait_soon(bars + 8u * stage, parity);
             const unsigned char* in = ring + (size_t)stage * stage_bytes;
@@ -170,18 +182,18 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
                 fetch_edge(row + 2 * rows);
             }
             if (OWNER == kCluster || kEdges) {
-                if (row + rows < a.N) next0 = to_float(__ldg(static_cast<const T*>(a.x) + (row + rows) * a.x_stride));
+                if (row + rows < a.N) fetch_head(static_cast<const T*>(a.x) + (row + rows) * a.x_stride);
             } else {
-                x0 = to_float(x[0]);
+                base = base_of(to_float(x[0]), to_float(x[second]), to_float(x[third]));
             }
-            if (!ok) x0 = __int_as_float(0x7fc00000);
+            if (!ok) base = __int_as_float(0x7fc00000);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 if (kEdges || has(k)) {
                     unpack<T, W>(load_packed<T, W>(x + (may_miss(k) ? min(first + k * step, words - 1) : first + k * step) * W), f[k]);
                     if (may_miss(k) && !has(k))
 #pragma unroll
-                        for (int j = 0; j < W; ++j) f[k][j] = x0;
+                        for (int j = 0; j < W; ++j) f[k][j] = base;
                 }
         } else {
 #pragma unroll
@@ -195,7 +207,7 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
             if (kEdges || has(k))
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
-                    f[k][j] -= x0;
+                    f[k][j] -= base;
                     s[(k * W + j) & 1] += f[k][j];
                 }
         float sum = s[0] + s[1], c = sum * over_n;
@@ -268,7 +280,7 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
         else if (a.y_type == ROCKET_F16) write(static_cast<__half*>(a.y));
         else write(static_cast<__nv_bfloat16*>(a.y));
         if (first == 0 && rank == 0) {
-            if (a.mean) a.mean[row + ahead] = x0 + mean;
+            if (a.mean) a.mean[row + ahead] = base + mean;
             if (a.rstd) a.rstd[row + ahead] = r;
         }
     }

@@ -1,10 +1,11 @@
 """Layer norm, forward and backward, against its definition in 64 bits.
 
-Tolerances, with u = 2^-24 (half a step of fp32) and h half a step of the output's type.  A kernel sums a row in chains of at
-most 64 fp32 additions joined by a tree of at most 16 levels, so a sum over a row is off by at most 80 u of the sum of
-magnitudes; wider sums are nearer.  With s the row's standard deviation, mean |x - m| <= s, so (x - m) r is off by at most 80 u
-through the mean, and relatively by 40 u through r (half the variance's 80 u) and 8 u through the roundings of a difference,
-two products and the root.  A sum over rows may be taken in any order: N u of the sum of magnitudes.
+Tolerances, with u = 2^-24 (half a step of fp32) and h half a step of the output's type.  A thread adds at most 32 values in two
+chains, 16 more additions join it to its warp, block and cluster: a sum over a row passes fewer than 40 roundings and is off by at
+most 40 u of the sum of magnitudes.  Where the rows are not far from zero, their mean (of values of up to |m| + s, with s the
+standard deviation) is off by at most 40 u (|m| + s), which is 80 u in units of s while |m| <= s; rows far from zero are taken
+relative to their first value.  r is off by 20 u through the variance's 40 u and by 8 u through the roundings of a difference, two
+products and the root: 48 u holds both.  A sum over rows may be taken in any order: N u of the sum of magnitudes.
 """
 import numpy as np
 import pytest
