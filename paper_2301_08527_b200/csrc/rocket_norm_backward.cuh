@@ -30,7 +30,7 @@ inline bool is_short(int P) { return P <= kWarpColumns; }
 inline int parts_of(int P) {
     const int fewest = (P + kThreads * kColumns - 1) / (kThreads * kColumns);
     if (fewest == 1) return 1;
-    for (int parts = fewest; parts < fewest + 3; ++parts) {
+    for (int parts = fewest; parts < fewest + 3 && parts <= kMostParts; ++parts) {
         const int part = ((P + parts - 1) / parts + 7) / 8 * 8, threads = round32((part + kColumns - 1) / kColumns);
         if (P - (parts - 1) * part >= (P % 4 ? kColumns - 1 : kColumns - 4) * threads) return parts;
     }
