@@ -25,6 +25,8 @@ constexpr int kWarpColumns = 32 * kColumns;
 constexpr int kSmemSm = 227 * 1024;       // shared memory of an SM
 
 inline bool is_short(int P) { return P <= kWarpColumns; }
+// Lanes of a short row: the fewest, since half of a warp's work would else be the sums' shuffles.
+inline int lanes_of(int P) { return P <= 8 * kColumns ? 8 : P <= 16 * kColumns ? 16 : 32; }
 // Blocks of a row: one or two more than the columns ask for where that gives all threads all words but the last (narrow words, of an odd P, are the harder to
 // divide).
 inline int parts_of(int P) {
@@ -46,7 +48,7 @@ inline bool is_long(int P) { return parts_of(P) > kMostParts; }
 inline int owners_of(int N, int P) {
     if (is_long(P)) return 0;
     if (N <= (is_short(P) ? 64 : 2)) return 1;           // no second launch: an owner by itself writes the gradients
-    const int rows = is_short(P) ? kThreads / 32 : 1;
+    const int rows = is_short(P) ? kThreads / lanes_of(P) : 1;
     return std::max(1, (int)std::min<int64_t>(((int64_t)N + rows - 1) / rows, (int64_t)kSms * resident_of(P) / (is_short(P) ? 1 : parts_of(P))));
 }
 
@@ -84,30 +86,33 @@ __device__ __forceinline__ void take(const float (&x)[W], const float (&dy)[W], 
     }
 }
 
-template <class TX, class TY, int W, int NV>
+// LANES of a warp share a row; a warp has 32 / LANES rows at a time, and its lanes for the same columns meet at the end.
+template <class TX, class TY, int W, int NV, int LANES>
 __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
     extern __shared__ float sums[];       // [2][P]
-    const int lane = threadIdx.x & 31, words = a.P / W;
-    const bool last = lane + 32 * (NV - 1) < words;
+    const int lane = threadIdx.x & (LANES - 1), ahead = (threadIdx.x & 31) / LANES, words = a.P / W;
+    const bool last = lane + LANES * (NV - 1) < words;
     auto has = [&](int k) { return k < NV - 1 || last; };
     float g[NV][W], dg[NV][W] = {}, db[NV][W] = {};
     Packed<TX, W> next_x[NV];
     Packed<TY, W> next_y[NV];
     float next_m = 0.0f, next_r = 0.0f;
     auto fetch = [&](int64_t n) {
+        n += ahead;
+        if (n >= a.N) return;
         const TX* __restrict__ x = static_cast<const TX*>(a.x) + n * a.x_stride + lane * W;
         const TY* __restrict__ dy = static_cast<const TY*>(a.dy) + n * a.dy_stride + lane * W;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (has(k)) {
-                next_x[k] = load_packed_once<TX, W>(x + 32 * k * W);
-                next_y[k] = load_packed_once<TY, W>(dy + 32 * k * W);
+                next_x[k] = load_packed_once<TX, W>(x + LANES * k * W);
+                next_y[k] = load_packed_once<TY, W>(dy + LANES * k * W);
             }
         next_m = __ldg(a.mean + n);
         next_r = __ldg(a.rstd + n);
     };
-    const int64_t rows = (int64_t)gridDim.x * (kThreads / 32);
-    int64_t row = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int64_t rows = (int64_t)gridDim.x * (kThreads / LANES);
+    int64_t row = (int64_t)blockIdx.x * (kThreads / LANES) + (threadIdx.x >> 5) * (32 / LANES);      // the warp's first
     if (row < a.N) fetch(row);
 #pragma unroll
     for (int k = 0; k < NV; ++k)
@@ -116,12 +121,13 @@ __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
     if (a.gamma)
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (has(k)) load_typed<W>(a.gamma, a.w_type, (lane + 32 * k) * W, g[k]);
+            if (has(k)) load_typed<W>(a.gamma, a.w_type, (lane + LANES * k) * W, g[k]);
     const float over_p = 1.0f / (float)a.P;
     for (; row < a.N; row += rows) {
         float xh[NV][W], u[NV][W];
         float2 s = make_float2(0.0f, 0.0f);
         const float m = next_m, r = next_r;
+        const bool mine = LANES == 32 || row + ahead < a.N;
         Packed<TX, W> cx[NV];
         Packed<TY, W> cy[NV];
 #pragma unroll
@@ -129,37 +135,46 @@ __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
         if (row + rows < a.N) fetch(row + rows);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (has(k)) {
+            if (has(k) && mine) {
                 float x[W], dy[W];
                 unpack<TX, W>(cx[k], x);
                 unpack<TY, W>(cy[k], dy);
                 take<W>(x, dy, g[k], m, r, xh[k], u[k], dg[k], db[k], s);
             }
-        s = row_sums<kWarp>(s, 0);
-        if (a.dx) {
+        s = LANES == 32 ? row_sums<kWarp>(s, 0) : make_float2(add_lanes(s.x, LANES / 2), add_lanes(s.y, LANES / 2));
+        if (a.dx && mine) {
             const float c1 = s.x * over_p * r, c2 = s.y * over_p * r;
-            TX* __restrict__ dx = static_cast<TX*>(a.dx) + row * a.dx_stride + lane * W;
+            TX* __restrict__ dx = static_cast<TX*>(a.dx) + (row + ahead) * a.dx_stride + lane * W;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 if (has(k)) {
                     float o[W];
 #pragma unroll
                     for (int j = 0; j < W; ++j) o[j] = fmaf(u[k][j], r, -fmaf(xh[k][j], c2, c1));
-                    store_packed<TX, W>(dx + 32 * k * W, o);
+                    store_packed<TX, W>(dx + LANES * k * W, o);
                 }
         }
     }
     asm volatile("griddepcontrol.launch_dependents;");      // the kernel that adds up the sums waits for this one's end
     if (!a.dgamma && !a.dbeta) return;
+#pragma unroll
+    for (int o = 16; o >= LANES; o /= 2)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                dg[k][j] += __shfl_xor_sync(0xffffffffu, dg[k][j], o);
+                db[k][j] += __shfl_xor_sync(0xffffffffu, db[k][j], o);
+            }
     // the warps add their sums in turn
     for (int w = 0; w < kThreads / 32; ++w) {
-        if ((int)(threadIdx.x >> 5) == w) {
+        if ((int)(threadIdx.x >> 5) == w && ahead == 0) {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 if (has(k))
 #pragma unroll
                     for (int j = 0; j < W; ++j) {
-                        const int p = (lane + 32 * k) * W + j;
+                        const int p = (lane + LANES * k) * W + j;
                         sums[p] = w == 0 ? dg[k][j] : sums[p] + dg[k][j];
                         sums[a.P + p] = w == 0 ? db[k][j] : sums[a.P + p] + db[k][j];
                     }
@@ -418,11 +433,16 @@ __global__ void __launch_bounds__(kLongThreads) long_weights_kernel(const Backwa
 
 template <class TX, class TY, int W>
 cudaError_t launch_short(const Backward& a, cudaStream_t stream) {
-    return with_int<1, kColumns / W>((a.P / W + 31) / 32, [&](auto nv) {
-        warp_rows_kernel<TX, TY, W, nv.value><<<owners_of(a.N, a.P), kThreads, 2 * a.P * sizeof(float), stream>>>(a);
-        count_launch();
-        return cudaGetLastError();
-    });
+    auto run = [&](auto lanes) {
+        constexpr int LANES = decltype(lanes)::value, kMost = kColumns / W;
+        return with_int<LANES == 8 ? 1 : kMost / 2 + 1, kMost>((a.P / W + LANES - 1) / LANES, [&](auto nv) {
+            warp_rows_kernel<TX, TY, W, nv.value, LANES><<<owners_of(a.N, a.P), kThreads, 2 * a.P * sizeof(float), stream>>>(a);
+            count_launch();
+            return cudaGetLastError();
+        });
+    };
+    const int lanes = lanes_of(a.P);
+    return lanes == 8 ? run(Int<8>()) : lanes == 16 ? run(Int<16>()) : run(Int<32>());
 }
 
 // owners: of at most so many, how many there are is put here.
