@@ -438,17 +438,6 @@ def _types():
     return _float_types
 
 
-def _on_device(call, device, where):
-    """Runs call(stream) with the device of that number current, on its current stream."""
-    if device == _current_device():
-        status = call(_current_stream())
-    else:
-        with _torch.cuda.device(device):
-            status = call(_current_stream())
-    if status:
-        raise RocketError(status, where)
-
-
 def _rows(t, name, shape=None, device=None, dtype=None):
     """(pointer, type code, row stride, N, P) of a CUDA tensor taken as rows of its last dimension: two dimensions with
     any distance between the rows, or any number of contiguous ones."""
@@ -512,6 +501,9 @@ def rocket_layer_norm(feat, gamma=None, beta=None, eps=1e-5, out=None, out_dtype
     torch = _t()
     x, xt, xs, N, P = _rows(feat, "feat")
     device, y = feat.get_device(), out
+    if device != _current_device():
+        with torch.cuda.device(device):
+            return rocket_layer_norm(feat, gamma, beta, eps, out, out_dtype, mean_out, rstd_out, want_stats)
     if y is not None:
         yp, yt, ys, _, _ = _rows(y, "out", feat.shape, device, out_dtype)
     else:
@@ -539,8 +531,9 @@ def rocket_layer_norm(feat, gamma=None, beta=None, eps=1e-5, out=None, out_dtype
     elif want_stats:
         rstd = torch.empty_like(mean)
         rp = rstd.data_ptr()
-    fn = (_lib or load_library()).rocket_layer_norm
-    _on_device(lambda s: fn(x, xt, xs, N, P, g, b, wt, eps, yp, yt, ys, mp, rp, s), device, "rocket_layer_norm")
+    status = (_lib or load_library()).rocket_layer_norm(x, xt, xs, N, P, g, b, wt, eps, yp, yt, ys, mp, rp, _current_stream())
+    if status:
+        raise RocketError(status, "rocket_layer_norm")
     return y, mean, rstd
 
 
@@ -552,6 +545,9 @@ def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dg
     f32 = torch.float32
     x, xt, xs, N, P = _rows(feat, "feat")
     device, place = feat.get_device(), feat.device
+    if device != _current_device():
+        with torch.cuda.device(device):
+            return rocket_layer_norm_backward(dy, feat, mean, rstd, gamma, dx_out, dgamma_out, dbeta_out, want_dx, want_weights, weight_dtype)
     d, yt, ds, _, _ = _rows(dy, "dy", feat.shape, device)
     mp = _vector(mean, N, "mean", device, f32)[0]
     rp = _vector(rstd, N, "rstd", device, f32)[0]
@@ -592,9 +588,9 @@ def rocket_layer_norm_backward(dy, feat, mean, rstd, gamma=None, dx_out=None, dg
         if need > 0:
             ws = torch.empty(need // 4, dtype=f32, device=place)
             wp = ws.data_ptr()
-    fn = lib.rocket_layer_norm_backward
-    _on_device(lambda s: fn(d, yt, ds, x, xt, xs, N, P, g, wt, mp, rp, dxp, dxs, dgp, dbp, wp, need, s), device,
-               "rocket_layer_norm_backward")
+    status = lib.rocket_layer_norm_backward(d, yt, ds, x, xt, xs, N, P, g, wt, mp, rp, dxp, dxs, dgp, dbp, wp, need, _current_stream())
+    if status:
+        raise RocketError(status, "rocket_layer_norm_backward")
     return dx, dg, db
 
 
@@ -639,36 +635,9 @@ def _address(a):
     return None if a is None else a.buffer_info()[0]
 
 
-def _norm_buffers(lib, count, sizes, grads, norm_out):
-    torch = _torch
-    f32 = torch.float32
-    place = grads[0].device if count else norm_out.device if norm_out is not None else torch.device("cuda", _current_device())
-    if norm_out is not None:
-        norm, np_ = norm_out, _vector(norm_out, 1, "norm_out", place.index, f32)[0]
-    else:
-        norm = torch.empty(1, dtype=f32, device=place)
-        np_ = norm.data_ptr()
-    need = lib.rocket_grad_norm_workspace(count, sizes)
-    ws = torch.empty(need // 4, dtype=f32, device=place) if need > 0 else None
-    return ws, ws.data_ptr() if need > 0 else None, need, norm, np_, place.index
-
-
-def rocket_grad_norm(grads, norm_out=None):
-    """2-norm of a gradient held in many tensors (a list or tuple of dense CUDA tensors of float32, float16 or bfloat16 on one
-    device).  Returns it as a [1] float32 tensor."""
-    n, ptrs, sizes, codes, _, _ = _tensor_list(grads, "grads")
-    lib = _lib or load_library()
-    p, z, c = _address(ptrs), _address(sizes), _address(codes)
-    ws, wp, need, norm, np_, device = _norm_buffers(lib, n, z, grads, norm_out)
-    _on_device(lambda s: lib.rocket_grad_norm(n, p, z, c, np_, wp, need, s), device, "rocket_grad_norm")
-    return norm
-
-
-def rocket_clip_grad_norm(grads, max_norm, out=None, norm_out=None):
-    """Scales the gradient by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of out (each with its gradient's
-    values in the same order, of its type or float32).  Returns (norm before clipping as a [1] float32 tensor, the clipped
-    tensors)."""
-    lib = _lib or load_library()
+def _norm_call(grads, max_norm, out, norm_out):
+    """Both norms; max_norm None: no clipping."""
+    torch = _t()
     n, ptrs, sizes, codes, device, contiguous = _tensor_list(grads, "grads")
     outs = out_codes = None
     if out is not None:
@@ -678,11 +647,44 @@ def rocket_clip_grad_norm(grads, max_norm, out=None, norm_out=None):
         if not (contiguous and out_contiguous) and any(
                 a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
             raise ValueError("out must have the shapes and strides of the gradients")
-    p, z, c, o, oc = _address(ptrs), _address(sizes), _address(codes), _address(outs), _address(out_codes)
-    ws, wp, need, norm, np_, device = _norm_buffers(lib, n, z, grads, norm_out)
-    _on_device(lambda s: lib.rocket_clip_grad_norm(n, p, z, c, o, oc, max_norm, np_, wp, need, s), device,
-               "rocket_clip_grad_norm")
-    return norm, grads if out is None else out
+    if n == 0:
+        device = norm_out.get_device() if isinstance(norm_out, torch.Tensor) and norm_out.is_cuda else _current_device()
+    if device != _current_device():
+        with torch.cuda.device(device):
+            return _norm_call(grads, max_norm, out, norm_out)
+    f32 = torch.float32
+    place = grads[0].device if n else torch.device("cuda", device)
+    if norm_out is not None:
+        norm, np_ = norm_out, _vector(norm_out, 1, "norm_out", device, f32)[0]
+    else:
+        norm = torch.empty(1, dtype=f32, device=place)
+        np_ = norm.data_ptr()
+    lib = _lib or load_library()
+    p, z, c = _address(ptrs), _address(sizes), _address(codes)
+    need, wp = lib.rocket_grad_norm_workspace(n, z), None
+    if need > 0:
+        ws = torch.empty(need // 4, dtype=f32, device=place)
+        wp = ws.data_ptr()
+    if max_norm is None:
+        status = lib.rocket_grad_norm(n, p, z, c, np_, wp, need, _current_stream())
+    else:
+        status = lib.rocket_clip_grad_norm(n, p, z, c, _address(outs), _address(out_codes), max_norm, np_, wp, need, _current_stream())
+    if status:
+        raise RocketError(status, "rocket_grad_norm" if max_norm is None else "rocket_clip_grad_norm")
+    return norm
+
+
+def rocket_grad_norm(grads, norm_out=None):
+    """2-norm of a gradient held in many tensors (a list or tuple of dense CUDA tensors of float32, float16 or bfloat16 on one
+    device).  Returns it as a [1] float32 tensor."""
+    return _norm_call(grads, None, None, norm_out)
+
+
+def rocket_clip_grad_norm(grads, max_norm, out=None, norm_out=None):
+    """Scales the gradient by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of out (each with its gradient's
+    values in the same order, of its type or float32).  Returns (norm before clipping as a [1] float32 tensor, the clipped
+    tensors)."""
+    return _norm_call(grads, float(max_norm), out, norm_out), grads if out is None else out
 
 
 def _host_ptr(t, dtype, name):
