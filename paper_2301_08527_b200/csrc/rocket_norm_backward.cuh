@@ -33,6 +33,7 @@ inline int lanes_of(int P) { return P <= 8 * kColumns ? 8 : P <= 16 * kColumns ?
 // Blocks of a row: one or two more than the columns ask for where that gives all threads all words but the last (narrow words, of an odd P, are the harder to
 // divide).
 inline int parts_of(int P) {
+    if (P > kMostParts * kThreads * kColumns) return kMostParts + 1;
     const int fewest = (P + kThreads * kColumns - 1) / (kThreads * kColumns);
     if (fewest == 1) return 1;
     for (int parts = fewest; parts < fewest + 3 && parts <= kMostParts; ++parts) {
@@ -461,6 +462,7 @@ cudaError_t launch_owners(const Backward& a, int& owners, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     const int stage = room_of(part, sizeof(TX)) + room_of(part, sizeof(TY));
     const int stages = std::min(kMostStages, (kSmemSm / resident_of(a.P) - 2048) / stage);      // 2 KB: the block's other arrays, and what the driver keeps
+    if (stages < 2) return cudaErrorInvalidConfiguration;      // the edges of a row are stored while the one before is read
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(owners * parts));
     cfg.blockDim = dim3((unsigned)threads);

@@ -391,6 +391,7 @@ cudaError_t launch_ring(const Forward& a, int threads, int parts, int resident, 
     if (e != cudaSuccess) return e;
     const int stage_words = (a.P / W + parts - 1) / parts, stage_bytes = room_of(stage_words * W, sizeof(T));
     const int stages = std::min(kMostStages, ring_bytes(resident) / stage_bytes);
+    if (stages < 2) return cudaErrorInvalidConfiguration;                // the edges of a row are stored while the one before is read
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(std::min(a.N, kSms * resident / parts) * parts));
     cfg.blockDim = dim3((unsigned)threads);
@@ -415,8 +416,16 @@ cudaError_t launch_ring(const Forward& a, int threads, int parts, int resident, 
     return cudaLaunchKernelEx(&cfg, kernel, a, parts, stages, stage_words);
 }
 
+template <class T>
+cudaError_t launch_long(const Forward& a, cudaStream_t stream) {
+    long_rows_kernel<T><<<(unsigned)a.N, kLongThreads, 0, stream>>>(a);
+    count_launch();
+    return cudaGetLastError();
+}
+
 template <class T, int W>
 cudaError_t launch_words(const Forward& a, cudaStream_t stream) {
+    if (a.P > 1 << 20) return launch_long<T>(a, stream);            // more than any cluster's registers hold; sums of sizes below fit into 32 bits
     const int words = a.P / W;
     // Short rows: as few lanes of a warp as hold the row in up to 16 values each (up to 20 in 16 lanes, 32 in 32), since half of a warp's work
     // would else be the sums' shuffles: 100,003 rows of 257 binary16 values take 28 us with 16 lanes and 31 with 32.
@@ -462,20 +471,14 @@ cudaError_t launch_words(const Forward& a, cudaStream_t stream) {
                          : launch_ring<T, W, kHeld, kCluster, kHold, kAny>(a, threads, blocks, resident, stream);
     }
     if constexpr (!kWide) {
-        long_rows_kernel<T><<<(unsigned)a.N, kLongThreads, 0, stream>>>(a);
-        count_launch();
-        return cudaGetLastError();
+        return launch_long<T>(a, stream);
     } else {
         // few rows: every thread reads its part of a row at once
         constexpr int kBlockWords = W == 8 ? 3 : 5;                 // of a thread
         int parts = 1;
         while (parts < kMostParts && (words > parts * 1024 * kBlockWords || ((int64_t)parts * a.N <= kSms && a.P >= parts * 2048))) parts *= 2;
         const int part = (words + parts - 1) / parts, least = words / parts;      // words of the blocks
-        if (part > 1024 * kBlockWords) {
-            long_rows_kernel<T><<<(unsigned)a.N, kLongThreads, 0, stream>>>(a);
-            count_launch();
-            return cudaGetLastError();
-        }
+        if (part > 1024 * kBlockWords) return launch_long<T>(a, stream);
         int nv = (part + 1023) / 1024;
         while (nv < kBlockWords && (part + nv - 1) / nv > 256 && nv * W < 16) ++nv;
         while (nv > 1 && (nv - 1) * round32((part + nv - 1) / nv) > least) --nv;

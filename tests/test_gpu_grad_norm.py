@@ -202,6 +202,17 @@ def test_captured_concurrent_and_the_same_bits_again(count, size):
         assert all(torch.equal(a, b) for a, b in zip(out, want_out))
 
 
+def test_a_tensor_of_more_values_than_32_bits_count():
+    torch = _torch()
+    n = (1 << 32) + 12345
+    g = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    ref = 0.5 * math.sqrt(n)
+    norm, _ = rk.rocket_clip_grad_norm([g, torch.zeros(7, device="cuda")], ref / 2)
+    assert abs(float(norm) - ref) <= 2 * U * ref
+    # 0.25 up to the 1e-6 beside the norm and fp32's roundings: the nearest bfloat16 value
+    assert float(g.min()) == 0.25 and float(g.max()) == 0.25
+
+
 def test_refusals_of_the_binding():
     torch = _torch()
     g = torch.randn((6, 8), device="cuda")

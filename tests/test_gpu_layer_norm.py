@@ -354,6 +354,27 @@ def test_gradients_against_differences():
             assert abs((args[0] - args[1]) / (2 * step) - grad[at]) <= 2e-3, (i, at)
 
 
+def test_offsets_beyond_32_bits():
+    torch = _torch()
+    N, P = 70000, 33001                          # 2.3e9 values, rows on every alignment
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    x = torch.randn((N, P), generator=gen, device="cuda", dtype=torch.bfloat16)
+    g = torch.rand(P, generator=gen, device="cuda") + 0.5
+    y, m, r = rk.rocket_layer_norm(x, g)
+    some = [0, 1, 32767, 65075, 65076, N - 2, N - 1]
+    for n in some:
+        _check_forward(x[n:n + 1], g, None, EPS, y[n:n + 1], m[n:n + 1], r[n:n + 1])
+    dx, dg, db = rk.rocket_layer_norm_backward(y, x, m, r, g)
+    for n in some:
+        _check_backward(y[n:n + 1], x[n:n + 1], m[n:n + 1], r[n:n + 1], g, dx[n:n + 1], None, None)
+    # the sums over all rows of the columns at both ends, any order: N u of the magnitudes
+    for c in (0, P - 1):
+        d, xh = _d(y[:, c]), (_d(x[:, c]) - _d(m)) * _d(r)
+        assert abs(float(dg[c]) - (d * xh).sum()) <= (N + 4) * U * np.abs(d * xh).sum()
+        assert abs(float(db[c]) - d.sum()) <= (N + 1) * U * np.abs(d).sum()
+
+
 # ---- how a program calls them --------------------------------------------------------------------------------------------
 
 SIZES = [(1, 20000), (32, 20000), (700, 1000), (5000, 64), (40, 70001)]

@@ -56,6 +56,11 @@ def test_backward_refuses(lib, kw):
     assert _backward(lib, **kw) == EINVAL
 
 
+@pytest.mark.parametrize("N,P", [(0, 1), (0x7fffffff, 1), (0x7fffffff, 512), (1, 0x7fffffff), (0x7fffffff, 0x7fffffff), (3, 65536), (3, 65537), (3, 0x7fffffff - 4000)])
+def test_workspace_sizes_at_the_ends(lib, N, P):
+    assert 0 <= lib.rocket_layer_norm_backward_workspace(N, P) < 1 << 30
+
+
 @pytest.mark.parametrize("N,P", [(1, 1), (32, 20000), (16384, 4096), (100003, 257), (5, 300000)])
 def test_backward_refuses_a_workspace_that_is_too_small(lib, N, P):
     need = lib.rocket_layer_norm_backward_workspace(N, P)
