@@ -76,7 +76,7 @@ __device__ __forceinline__ int tensor_of(const Table<N>& t, int64_t value) {
 }
 
 // Calls f(tensor, position in it, how many) for the pieces of this block's share of the line, a contiguous one.  Shares begin at multiples of
-// 64 values, which keeps them on 16-byte borders where the tensors are.
+// 64 values, on 16-byte borders where the tensors begin and end on such.
 template <int N, class F>
 __device__ __forceinline__ void for_share(const Table<N>& t, int block, int blocks, F&& f) {
     const int64_t total = t.first[t.tensors], units = (total + 63) / 64;
