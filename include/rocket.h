@@ -299,7 +299,7 @@ int rocket_layer_norm(const void* x_dev, int x_type, int64_t x_stride, int N, in
  *   dx_dev [N][P] of x_type, rows dx_stride apart; dgamma_dev, dbeta_dev [P] of w_type; each assigned (not accumulated), or
  *   left out where it is NULL (not all three)
  *   workspace_dev  workspace_bytes >= rocket_layer_norm_backward_workspace(N, P) (which is ROCKET_EINVAL for sizes out of
- *   range) where dgamma or dbeta is wanted; else, or where that is 0, it may be NULL
+ *   range) where dgamma or dbeta is wanted; else, or where that is 0 (as it is for few rows), it may be NULL
  * The same call gives the same bits each time.  N = 0 writes zeros to dgamma and dbeta.  Errors as in the forward.
  */
 int64_t rocket_layer_norm_backward_workspace(int N, int P);

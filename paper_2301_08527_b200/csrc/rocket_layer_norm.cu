@@ -107,6 +107,6 @@ extern "C" int rocket_layer_norm_backward(const void* dy_dev, int y_type, int64_
     }
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const norm::Backward a = {dy_dev, x_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, dgamma_dev, dbeta_dev, static_cast<float*>(workspace_dev),
-                              dy_stride, x_stride, dx_stride, N, P, y_type, x_type, w_type};
+                              dy_stride, x_stride, dx_stride, N, P, y_type, x_type, w_type, false};
     return status_of(norm::launch_backward(a, stream));
 }

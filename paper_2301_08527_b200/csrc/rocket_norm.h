@@ -34,6 +34,7 @@ struct Backward {
     float* partial;       // workspace
     int64_t dy_stride, x_stride, dx_stride;
     int N, P, y_type, x_type, w_type;
+    bool joined;          // the owners' sums meet in a cluster
 };
 
 // Bytes of workspace for the gradients of gamma and beta.

@@ -48,12 +48,20 @@ inline int threads_of(int P) { return round32((part_of(P) + kColumns - 1) / kCol
 inline int resident_of(int P) { return is_short(P) ? 2 : std::min(512 / threads_of(P), 16); }
 inline bool is_long(int P) { return parts_of(P) > kMostParts; }
 
-// Owners whose sums go to the workspace (a block of warps adds its own up first).
+// Rows that a block has at a time.
+inline int block_rows(int P) { return is_short(P) ? kThreads / lanes_of(P) : 1; }
+// Few rows: the blocks of one cluster are all owners, and add their sums up in distributed shared memory: no workspace, and no second launch.
+// Up to so many turns of each: 32 rows of 1,000 columns take 4.6 us of device time so and 4.0 with a second kernel, 128 rows 8.5 and 4.3, but that kernel's
+// launch and workspace cost the caller 4.3.
+constexpr int kJoinedTurns = 8;
+inline bool is_joined(int N, int P) { return parts_of(P) == 1 && N <= (int64_t)kMostParts * block_rows(P) * kJoinedTurns; }
+
+// Owners of rows (a block of warps adds its own sums up first).
 inline int owners_of(int N, int P) {
     if (is_long(P)) return 0;
-    if (N <= (is_short(P) ? 64 : 2)) return 1;           // no second launch: an owner by itself writes the gradients
-    const int rows = is_short(P) ? kThreads / lanes_of(P) : 1;
-    return std::max(1, (int)std::min<int64_t>(((int64_t)N + rows - 1) / rows, (int64_t)kSms * resident_of(P) / (is_short(P) ? 1 : parts_of(P))));
+    if (parts_of(P) > 1 && N <= 2) return 1;             // a cluster by itself writes the gradients
+    const int64_t want = ((int64_t)N + block_rows(P) - 1) / block_rows(P);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(want, is_joined(N, P) ? kMostParts : kSms * resident_of(P) / (is_short(P) ? 1 : parts_of(P))));
 }
 
 // Sums of two values over the threads that own a row, the same bits in each.  Each half of a warp goes on with one of the values, which saves
@@ -75,6 +83,26 @@ __device__ __forceinline__ float2 row_sums(float2 v, int turn) {
     return make_float2(__shfl_sync(0xffffffffu, s, 0), __shfl_sync(0xffffffffu, s, 16));
 }
 
+// dg and db from the sums [2][P] that every block of a cluster has in shared memory: each block adds up a share of the columns, in the blocks' order.
+__device__ __forceinline__ void join_owners(const float* sums, const Backward& a) {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const int blocks = gridDim.x;
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < 2 * a.P; i += blocks * blockDim.x) {
+        float v[1] = {0.0f};
+        for (int b = 0; b < blocks; ++b) {
+            uint32_t from;
+            float x;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(fast::smem_u32(sums + i)), "r"(b));
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(from) : "memory");
+            v[0] += x;
+        }
+        void* out = i < a.P ? a.dgamma : a.dbeta;
+        if (out) store_typed<1>(out, a.w_type, i < a.P ? i : i - a.P, v);
+    }
+    leave_cluster();                      // the others may still read this block's sums
+}
+
 // One row's work of a thread: xh and u from x and dy, the sums over the row, the sums over the rows.
 template <int W>
 __device__ __forceinline__ void take(const float (&x)[W], const float (&dy)[W], const float (&g)[W], float m, float r, float (&xh)[W], float (&u)[W],
@@ -93,7 +121,7 @@ __device__ __forceinline__ void take(const float (&x)[W], const float (&dy)[W], 
 // LANES of a warp share a row; a warp has 32 / LANES rows at a time, and its lanes for the same columns meet at the end.
 template <class TX, class TY, int W, int NV, int LANES>
 __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
-    extern __shared__ float sums[];       // [2][P]
+    extern __shared__ float sums[];       // of every warp, [2][P]
     const int lane = threadIdx.x & (LANES - 1), ahead = (threadIdx.x & 31) / LANES, words = a.P / W;
     const bool last = lane + LANES * (NV - 1) < words;
     auto has = [&](int k) { return k < NV - 1 || last; };
@@ -170,30 +198,27 @@ __global__ void __launch_bounds__(kThreads) warp_rows_kernel(const Backward a) {
                 dg[k][j] += __shfl_xor_sync(0xffffffffu, dg[k][j], o);
                 db[k][j] += __shfl_xor_sync(0xffffffffu, db[k][j], o);
             }
-    // the warps add their sums in turn
-    for (int w = 0; w < kThreads / 32; ++w) {
-        if ((int)(threadIdx.x >> 5) == w && ahead == 0) {
+    // every warp's sums, then those of the block in the first one's place
+    float* own = sums + (threadIdx.x >> 5) * 2 * a.P;
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (has(k))
+    for (int k = 0; k < NV; ++k)
+        if (has(k) && ahead == 0)
 #pragma unroll
-                    for (int j = 0; j < W; ++j) {
-                        const int p = (lane + LANES * k) * W + j;
-                        sums[p] = w == 0 ? dg[k][j] : sums[p] + dg[k][j];
-                        sums[a.P + p] = w == 0 ? db[k][j] : sums[a.P + p] + db[k][j];
-                    }
-        }
-        __syncthreads();
+            for (int j = 0; j < W; ++j) {
+                const int p = (lane + LANES * k) * W + j;
+                own[p] = dg[k][j];
+                own[a.P + p] = db[k][j];
+            }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.P; i += kThreads) {
+        float v = sums[i];
+#pragma unroll
+        for (int w = 1; w < kThreads / 32; ++w) v += sums[w * 2 * a.P + i];
+        sums[i] = v;
     }
-    if (gridDim.x == 1) {
-        for (int i = threadIdx.x; i < a.P; i += kThreads) {
-            if (a.dgamma) store_typed<1>(a.dgamma, a.w_type, i, {sums[i]});
-            if (a.dbeta) store_typed<1>(a.dbeta, a.w_type, i, {sums[a.P + i]});
-        }
-        return;
-    }
+    if (a.joined) return join_owners(sums, a);
     float* out = a.partial + (int64_t)blockIdx.x * 2 * a.P;
-    for (int i = threadIdx.x; i < 2 * a.P; i += kThreads) out[i] = sums[i];
+    for (int i = threadIdx.x; i < 2 * a.P; i += kThreads) out[i] = sums[i];      // the thread's own
 }
 
 // A block's part of every row of its owner's; the rows come by bulk copies, as many ahead as there are stages.
@@ -344,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
     if constexpr (OWNER == kCluster) leave_cluster();
     asm volatile("griddepcontrol.launch_dependents;");
     if (!a.dgamma && !a.dbeta) return;
-    if (owners == 1) {
+    if (OWNER == kCluster && owners == 1) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (has(k)) {
@@ -353,7 +378,8 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
             }
         return;
     }
-    float* out = a.partial + (int64_t)owner * 2 * a.P + beg;
+    // where the owners are joined, their sums take the place of the rows (which no thread reads any more, nor any copy writes)
+    float* out = a.joined ? reinterpret_cast<float*>(ring) : a.partial + (int64_t)owner * 2 * a.P + beg;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         if (has(k))
@@ -363,6 +389,7 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
                 out[p] = dg[k][j];
                 out[a.P + p] = db[k][j];
             }
+    if (OWNER == kBlock && a.joined) join_owners(out, a);
 }
 
 // ---- rows longer than a cluster's registers: a block per row, then a block per 32 columns, sums in double precision ------------------
@@ -435,14 +462,35 @@ __global__ void __launch_bounds__(kLongThreads) long_weights_kernel(const Backwa
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------------------
 
+// Launches a kernel of `owners` blocks, as one cluster where they are joined.
+template <class... A, class... B>
+cudaError_t launch_joined(void (*kernel)(A...), std::atomic<uint64_t>& done, int owners, int threads, size_t bytes, bool joined, cudaStream_t stream, B... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)owners);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)owners;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = joined ? 1 : 0;
+    if (joined && owners > 8) {
+        const cudaError_t e = once_per_device(done, [&] { return allow_large_clusters(kernel); });
+        if (e != cudaSuccess) return e;
+    }
+    count_launch();
+    return cudaLaunchKernelEx(&cfg, kernel, A(args)...);
+}
+
 template <class TX, class TY, int W>
 cudaError_t launch_short(const Backward& a, cudaStream_t stream) {
     auto run = [&](auto lanes) {
         constexpr int LANES = decltype(lanes)::value, kMost = kColumns / W;
         return with_int<LANES == 8 ? 1 : kMost / 2 + 1, kMost>((a.P / W + LANES - 1) / LANES, [&](auto nv) {
-            warp_rows_kernel<TX, TY, W, nv.value, LANES><<<owners_of(a.N, a.P), kThreads, 2 * a.P * sizeof(float), stream>>>(a);
-            count_launch();
-            return cudaGetLastError();
+            static std::atomic<uint64_t> done{0};
+            return launch_joined(warp_rows_kernel<TX, TY, W, nv.value, LANES>, done, owners_of(a.N, a.P), kThreads, (size_t)(kThreads / 32) * 2 * a.P * sizeof(float), a.joined, stream, a);
         });
     };
     const int lanes = lanes_of(a.P);
@@ -457,7 +505,7 @@ cudaError_t launch_owners(const Backward& a, int& owners, cudaStream_t stream) {
     static std::atomic<uint64_t> done{0};
     cudaError_t e = once_per_device(done, [&] {
         const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemSm - 4096);
-        return set == cudaSuccess && OWNER == kCluster ? allow_large_clusters(kernel) : set;
+        return set == cudaSuccess ? allow_large_clusters(kernel) : set;
     });
     if (e != cudaSuccess) return e;
     const int stage = room_of(part, sizeof(TX)) + room_of(part, sizeof(TY));
@@ -470,10 +518,10 @@ cudaError_t launch_owners(const Backward& a, int& owners, cudaStream_t stream) {
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)parts;
+    attr[0].val.clusterDim.x = (unsigned)(OWNER == kCluster ? parts : owners);
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = OWNER == kCluster ? 1 : 0;
+    cfg.numAttrs = OWNER == kCluster || a.joined ? 1 : 0;
     if constexpr (OWNER == kCluster) {
         // not every SM finds partners in its group of SMs: clusters that would have to wait for others to end cost a second round
         static std::atomic<int> known[kMostParts + 1][kThreads / 32 + 1];
