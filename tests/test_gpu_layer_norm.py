@@ -377,7 +377,7 @@ def test_offsets_beyond_32_bits():
 
 # ---- how a program calls them --------------------------------------------------------------------------------------------
 
-SIZES = [(1, 20000), (32, 20000), (700, 1000), (5000, 64), (40, 70001)]
+SIZES = [(1, 20000), (32, 20000), (700, 1000), (100, 1000), (5000, 64), (500, 65), (40, 70001)]
 
 
 @pytest.mark.parametrize("N,P", SIZES)
