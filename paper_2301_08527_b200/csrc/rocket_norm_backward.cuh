@@ -290,10 +290,11 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (has(k)) load_typed<W>(a.gamma, a.w_type, beg + (first + k * step) * W, g[k]);
-    // nobody waits on a barrier, or writes to another block's shared memory, before it is there
+    // Nobody waits on a barrier, or writes to another block's shared memory, before it is there, nor reads the first row before its edges are: the
+    // arrival releases the stores above.
     if constexpr (OWNER == kCluster) {
         exchange.init();
-        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     } else {
         __syncthreads();

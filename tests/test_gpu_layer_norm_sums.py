@@ -1,0 +1,58 @@
+"""Layer norm backward with inputs of small whole numbers, mean 0 and rstd 1: then dgamma = sum dy x and dbeta = sum dy are whole numbers
+below 2^24, which fp32 holds in whatever order they are added, and one lost, doubled or stale row shows in every column."""
+import numpy as np
+import pytest
+
+import paper_2301_08527_b200 as rk
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _type(name):
+    torch = _torch()
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def _whole(gen, N, P, dtype, at, pad, most):
+    """[N, P] of -most .. most, the first row `at` values behind a 16-byte border, rows `pad` values apart."""
+    torch = _torch()
+    buf = torch.empty(at + N * (P + pad), dtype=dtype, device="cuda")
+    v = buf[at:].view(N, P + pad)[:, :P]
+    v.copy_(torch.randint(-most, most + 1, (N, P), generator=gen, device="cuda"))
+    return v
+
+
+def _unit(N):
+    torch = _torch()
+    return torch.zeros(N, device="cuda"), torch.ones(N, device="cuda")
+
+
+def _check_dx(dx, dy, x):
+    # as rounded: u = dy, xh = x and the sums over a row are whole and exact; 1/P, two products and two sums of fp32 follow (8 u holds them)
+    d, v = dy.double(), x.double()
+    c1, c2 = d.mean(1, keepdim=True), (d * v).mean(1, keepdim=True)
+    ref = d - c1 - v * c2
+    h = _torch().finfo(dx.dtype).eps / 2
+    tol = 8 * U * (d.abs() + c1.abs() + (v * c2).abs()) * (1 + h) + h * ref.abs() + 2.0 ** -25
+    assert bool(((dx.double() - ref).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("N", [1, 2, 3, 40])
+@pytest.mark.parametrize("P", [4097, 5003, 9997, 20003, 33001, 65535])
+@pytest.mark.parametrize("x,y", [("f32", "f32"), ("bf16", "f16"), ("f32", "bf16")])
+def test_first_rows_of_every_owner_at_any_alignment(N, P, x, y):
+    gen = _torch().Generator(device="cuda")
+    gen.manual_seed(P + N)
+    for k in range(6):                          # other values each time: what a block's shared memory held before shows
+        feat, dy = _whole(gen, N, P, _type(x), k % 4, k, 3), _whole(gen, N, P, _type(y), (k + 1) % 8, 1, 3)
+        dx, dg, db = rk.rocket_layer_norm_backward(dy, feat, *_unit(N))
+        assert np.array_equal(dg.double().cpu().numpy(), (dy.double() * feat.double()).sum(0).cpu().numpy())
+        assert np.array_equal(db.double().cpu().numpy(), dy.double().sum(0).cpu().numpy())
+        _check_dx(dx, dy, feat)
