@@ -89,6 +89,8 @@ __device__ __forceinline__ void join_owners(const float* sums, const Backward& a
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     const int blocks = gridDim.x;
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < 2 * a.P; i += blocks * blockDim.x) {
+        void* out = i < a.P ? a.dgamma : a.dbeta;
+        if (!out) continue;
         float v[1] = {0.0f};
         for (int b = 0; b < blocks; ++b) {
             uint32_t from;
@@ -97,10 +99,11 @@ __device__ __forceinline__ void join_owners(const float* sums, const Backward& a
             asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(from) : "memory");
             v[0] += x;
         }
-        void* out = i < a.P ? a.dgamma : a.dbeta;
-        if (out) store_typed<1>(out, a.w_type, i < a.P ? i : i - a.P, v);
+        store_typed<1>(out, a.w_type, i < a.P ? i : i - a.P, v);
     }
-    leave_cluster();                      // the others may still read this block's sums
+    // no block ends while another still reads its sums: the arrival stands behind the reads
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // One row's work of a thread: xh and u from x and dy, the sums over the row, the sums over the rows.

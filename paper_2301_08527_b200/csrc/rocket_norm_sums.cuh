@@ -109,7 +109,8 @@ struct Exchange {
     }
 };
 
-// No block of a cluster ends while another may still write to its shared memory.
+// No block of a cluster ends while another may still write to its shared memory.  (Each has what was sent to it before it arrives; a block that
+// still reads another's memory needs an arrival that releases.)
 __device__ __forceinline__ void leave_cluster() {
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");

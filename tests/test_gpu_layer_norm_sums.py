@@ -56,3 +56,19 @@ def test_first_rows_of_every_owner_at_any_alignment(N, P, x, y):
         assert np.array_equal(dg.double().cpu().numpy(), (dy.double() * feat.double()).sum(0).cpu().numpy())
         assert np.array_equal(db.double().cpu().numpy(), dy.double().sum(0).cpu().numpy())
         _check_dx(dx, dy, feat)
+
+
+@pytest.mark.parametrize("N,P", [(1, 7), (2, 4096), (5, 600), (16, 1001), (40, 513), (300, 40), (500, 257)])
+def test_one_of_the_sums_of_few_rows(N, P):
+    torch = _torch()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N)
+    for _ in range(20):
+        feat, dy = _whole(gen, N, P, torch.float32, 0, 0, 3), _whole(gen, N, P, torch.float32, 0, 0, 3)
+        wg, wb = (dy.double() * feat.double()).sum(0).float(), dy.double().sum(0).float()
+        _, dg, db = rk.rocket_layer_norm_backward(dy, feat, *_unit(N), want_dx=False, want_weights=False, dgamma_out=torch.empty(P, device="cuda"))
+        assert db is None and torch.equal(dg, wg)
+        _, dg, db = rk.rocket_layer_norm_backward(dy, feat, *_unit(N), want_dx=False, want_weights=False, dbeta_out=torch.empty(P, device="cuda"))
+        assert dg is None and torch.equal(db, wb)
+        _, dg, db = rk.rocket_layer_norm_backward(dy, feat, *_unit(N))
+        assert torch.equal(dg, wg) and torch.equal(db, wb)

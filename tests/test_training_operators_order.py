@@ -27,3 +27,11 @@ def test_the_edges_of_the_first_row_are_there_before_it_is_read():
     body = _body("rocket_norm_forward.cuh", "rows_kernel(const Forward a")
     between = body[body.index("edge.put(ring);"):body.index("for (int turn = 0; row < a.N")]
     assert re.search(r"if constexpr \(OWNER != kWarp\) \{[^}]*__syncthreads\(\);", between)
+
+
+def test_no_block_ends_while_another_reads_its_sums():
+    # every value loaded from another block is used, and the last arrival releases, so that it stands behind the loads
+    body = _body("rocket_norm_backward.cuh", "join_owners(const float* sums")
+    loop, end = body[body.index("for (int i ="):body.rindex("store_typed")], body[body.rindex("store_typed"):]
+    assert loop.index("if (!out) continue;") < loop.index("ld.shared::cluster")
+    assert "leave_cluster" not in end and "barrier.cluster.arrive.release" in end and "barrier.cluster.wait.acquire" in end
