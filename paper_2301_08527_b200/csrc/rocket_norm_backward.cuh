@@ -335,7 +335,6 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
                     for (int j = 0; j < W; ++j) { x[j] = m; dy[j] = 0.0f; }
                 take<W>(x, dy, g[k], m, r, xh[k], u[k], dg[k], db[k], s);
             }
-        if (!ok) dg[0][0] = db[0][0] = s.x;
         // behind the reduction's first barrier everybody has read the row: the next one may come into its place
         s = row_sums<OWNER>(s, turn);
         if (threadIdx.x == 0 && ok && to_copy < a.N) {
@@ -364,6 +363,11 @@ __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward 
         m = next_m;
         r = next_r;
     }
+    if (!ok)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < W; ++j) dg[k][j] = db[k][j] = __int_as_float(0x7fc00000);
     // copies that a wait gave up on must not outlive the block
     if (threadIdx.x == 0 && !ok)
         for (int s = 0; s < stages; ++s) {

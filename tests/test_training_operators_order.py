@@ -35,3 +35,9 @@ def test_no_block_ends_while_another_reads_its_sums():
     loop, end = body[body.index("for (int i ="):body.rindex("store_typed")], body[body.rindex("store_typed"):]
     assert loop.index("if (!out) continue;") < loop.index("ld.shared::cluster")
     assert "leave_cluster" not in end and "barrier.cluster.arrive.release" in end and "barrier.cluster.wait.acquire" in end
+
+
+def test_a_wait_that_gave_up_shows_in_every_sum_of_its_thread():
+    body = _body("rocket_norm_backward.cuh", "block_rows_kernel(const Backward a")
+    behind = body[body.index("m = next_m;"):body.index("float* out = a.joined")]
+    assert re.search(r"if \(!ok\).*k < NV.*dg\[k\]\[j\] = db\[k\]\[j\] = __int_as_float\(0x7fc00000\)", behind, re.S)
