@@ -229,7 +229,7 @@ template <class TX, class TY, int W, int NV, Owner OWNER, Fit FIT>
 __global__ void __launch_bounds__(kThreads, 2) block_rows_kernel(const Backward a, int parts, int part, int stages) {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ __align__(8) uint64_t arrived[kMostStages];
-    __shared__ Exchange exchange;
+    __shared__ Exchange<float2> exchange;
     const int rank = OWNER == kCluster ? blockIdx.x % parts : 0, owner = blockIdx.x / parts, owners = gridDim.x / parts;
     const int beg = rank * part, columns = min(part, a.P - beg), words = columns / W, first = threadIdx.x, step = blockDim.x;
     const bool last = first + (NV - 1) * step < words;

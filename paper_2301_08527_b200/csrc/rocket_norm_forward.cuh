@@ -1,11 +1,12 @@
 // Layer norm forward: m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), y = (x - m) r g + b for every row.
 //
-// Bound: memory.  A row is read once and stays in registers while its owner's next row is on its way.  All is relative to a base: the row's
-// first value where the first three lie close together beside their distance from zero, as in a row far from zero or a constant one, whose
-// differences are then exact, else 0, which leaves small means exact.  A thread takes the mean c of its values and the sum q of their squared
-// distances from c; where sets of values meet, with n, c and q each, the whole has c = sum n c / sum n and q = sum (q + n (c - whole's c)^2).
-// So the second moment is never a difference of large numbers, and the threads of a block need one barrier, the blocks of a cluster one exchange
-// per row.
+// Bound: memory.  A row is read once and stays in registers while its owner's next row is on its way.  A thread takes the mean of its values,
+// as c + l with l a rounding of c (from the differences to its first value, which are exact where the row is far from zero), keeps the values as
+// d = x - c, and takes the sum q of d^2.  Where sets of values meet, with n, mean and q each, the whole has the mean sum n c / sum n and
+// q = sum (q + n (c - whole's c)^2) (Chan, Golub and LeVeque); means are handed on as such pairs and added up as differences to the first set's.  So
+// everything is held by its distance from a mean of some of the row's values, d + (c - mean) is y's numerator, and neither a row's distance from
+// zero nor single values unlike the others cost the rest their digits; the threads of a block need one barrier, the blocks of a cluster one
+// exchange per row.
 //
 // Who has a row: a warp where it is short, a block, or the blocks of a cluster where rows are few or longer than a block's
 // registers.  The owners stay and go through the rows in turn.
@@ -16,6 +17,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cfloat>
 
 #include "rocket_float_types.cuh"
 #include "rocket_internal.h"
@@ -34,11 +36,10 @@ constexpr int kSmemSm = 227 * 1024;       // shared memory of an SM
 
 // Threads that hold gamma and beta: 32 values of each, or 16 where they are loaded one by one; most threads of a block, and of one in a cluster.
 constexpr int held_values(int W) { return W == 1 ? 16 : 32; }
-constexpr int hold_threads(Owner owner, int values) { return values < 16 ? 1024 : (owner == kCluster ? 160 : 128) * (32 / values); }
+__host__ __device__ constexpr int hold_threads(Owner owner, int values) { return values < 16 ? 1024 : (owner == kCluster ? 160 : 128) * (32 / values); }
 
-__device__ __forceinline__ float base_of(float a, float b, float c) {
-    const float near = 0.25f * fabsf(a);
-    return fabsf(b - a) <= near && fabsf(c - a) <= near ? a : 0.0f;
+__host__ __device__ constexpr int most_threads(Owner owner, Weights weights, int values) {
+    return owner == kWarp ? 256 : weights == kHold ? hold_threads(owner, values) : 1024;
 }
 
 // Blocks of an SM that the registers are cut for.
@@ -50,14 +51,13 @@ constexpr int resident_blocks(Owner owner, Weights weights, int values) {
 // thread that gives up waiting counts as NaN, which makes the row NaN); else the threads hold the next one in registers.  LANES of a warp share a
 // row; a warp has 32 / LANES rows at a time.
 template <class T, int W, int NV, Owner OWNER, Weights WEIGHTS, Fit FIT, bool RING = false, int LANES = 32>
-__global__ void __launch_bounds__(OWNER == kWarp ? 256 : WEIGHTS == kHold ? hold_threads(OWNER, NV * W) : 1024,
-                                  resident_blocks(OWNER, WEIGHTS, NV * W))
+__global__ void __launch_bounds__(most_threads(OWNER, WEIGHTS, NV * W), resident_blocks(OWNER, WEIGHTS, NV * W))
 rows_kernel(const Forward a, int parts, int stages, int stage_words) {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ __align__(8) uint64_t arrived[RING ? kMostStages : 1];
     int64_t row, rows;
     int beg = 0, words = a.P / W, first, step, rank = 0;
-    __shared__ Exchange exchange;
+    __shared__ Exchange<float4> exchange;
     if constexpr (OWNER == kWarp) {
         row = (int64_t)blockIdx.x * (blockDim.x / LANES) + (threadIdx.x >> 5) * (32 / LANES);      // the warp's first; its lanes' below
         rows = (int64_t)gridDim.x * (blockDim.x / LANES);
@@ -80,16 +80,9 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
     const bool last = first + (NV - 1) * step < words;
     auto has = [&](int k) { return FIT == kFull || (FIT == kAny ? first + k * step < words : k < NV - 1 || last); };
     constexpr bool kEdges = RING && (FIT == kAny || FIT == kEnd);
-    auto may_miss = [](int k) { return kEdges && (FIT == kAny || k == NV - 1); };      // read all the same, as the base
+    auto may_miss = [](int k) { return kEdges && (FIT == kAny || k == NV - 1); };      // read all the same, and counted as nothing
     const int at = beg + first * W;
     Packed<T, W> next[RING ? 1 : NV];
-    T next_head[3] = {};                                   // the next row's first values
-    const int second = min(1, a.P - 1), third = min(2, a.P - 1);
-    auto fetch_head = [&](const T* x) {
-        next_head[0] = __ldg(x);
-        next_head[1] = __ldg(x + second);
-        next_head[2] = __ldg(x + third);
-    };
     const int ahead = OWNER == kWarp ? (threadIdx.x & 31) / LANES : 0;
     const T* source = static_cast<const T*>(a.x) + (row + ahead) * a.x_stride;
     const int64_t source_step = rows * a.x_stride;
@@ -99,7 +92,6 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (has(k)) next[RING ? 0 : k] = load_packed_once<T, W>(from + k * step * W);
-        fetch_head(source);
         source += source_step;
     };
     const uint32_t bars = fast::smem_u32(arrived), rings = fast::smem_u32(ring), stage_bytes = (uint32_t)room_of(stage_words * W, sizeof(T));
@@ -137,7 +129,6 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
             edge.put(ring);
             fetch_edge(row + rows);
         }
-        if ((OWNER == kCluster || kEdges) && row < a.N) fetch_head(static_cast<const T*>(a.x) + row * a.x_stride);
     } else {
         if (row < a.N) fetch(row);
     }
@@ -154,27 +145,27 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
     const int n_thread = ((words - first + step - 1) / step) * W;
     const float n = (float)(words > first ? n_thread : 0), over_n = n > 0.0f ? 1.0f / n : 0.0f;
     const float n_warp = add_lanes(n, LANES / 2), over_warp = n_warp > 0.0f ? 1.0f / n_warp : 0.0f;
-    __shared__ float warp_n[32];
-    float n_lane = 0.0f, over_lane = 0.0f;
+    constexpr int kMostWarps = most_threads(OWNER, WEIGHTS, NV * W) / 32;
+    __shared__ float warp_n[kMostWarps];
+    const int warps = blockDim.x >> 5;
+    float n_lane = 0.0f;
     if constexpr (OWNER != kWarp) {
         if ((threadIdx.x & 31) == 0) warp_n[threadIdx.x >> 5] = n_warp;
         __syncthreads();
-        n_lane = (threadIdx.x & 31) < (blockDim.x >> 5) ? warp_n[threadIdx.x & 31] : 0.0f;
-        over_lane = n_lane > 0.0f ? 1.0f / n_lane : 0.0f;
+        n_lane = (threadIdx.x & 31) < warps ? warp_n[threadIdx.x & 31] : 0.0f;
     }
     const float over_block = 1.0f / (float)(words * W), over_p = 1.0f / (float)a.P;
     // the cluster's blocks, a lane for each in both halves of a warp
     const int part_lane = threadIdx.x & (kMostParts - 1);
-    float n_part = 0.0f, over_part = 0.0f;
+    float n_part = 0.0f;
     if (OWNER == kCluster && part_lane < parts) {
         const int64_t all = a.P / W;
         n_part = (float)(((int)(all * (part_lane + 1) / parts) - (int)(all * part_lane / parts)) * W);
-        over_part = 1.0f / n_part;
     }
     if constexpr (OWNER == kCluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     bool ok = true;
     for (int turn = 0; row < a.N; row += rows, ++turn) {
-        float f[NV][W], base = base_of(to_float(next_head[0]), to_float(next_head[1]), to_float(next_head[2]));
+        float f[NV][W];
         if constexpr (RING) {
             ok = ok && wait_soon(bars + 8u * stage, parity);
             const unsigned char* in = ring + (size_t)stage * stage_bytes;
@@ -184,19 +175,13 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
                 edge.put(ring + (size_t)(stage + 1 == stages ? 0 : stage + 1) * stage_bytes);
                 fetch_edge(row + 2 * rows);
             }
-            if (OWNER == kCluster || kEdges) {
-                if (row + rows < a.N) fetch_head(static_cast<const T*>(a.x) + (row + rows) * a.x_stride);
-            } else {
-                base = base_of(to_float(x[0]), to_float(x[second]), to_float(x[third]));
-            }
-            if (!ok) base = __int_as_float(0x7fc00000);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 if (kEdges || has(k)) {
                     unpack<T, W>(load_packed<T, W>(x + (may_miss(k) ? min(first + k * step, words - 1) : first + k * step) * W), f[k]);
                     if (may_miss(k) && !has(k))
 #pragma unroll
-                        for (int j = 0; j < W; ++j) f[k][j] = base;
+                        for (int j = 0; j < W; ++j) f[k][j] = f[0][0];
                 }
         } else {
 #pragma unroll
@@ -204,32 +189,34 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
                 if (has(k)) unpack<T, W>(next[RING ? 0 : k], f[k]);
             if (row + rows < a.N) fetch(row + rows);
         }
+        // the thread's mean c + l, from its first value on
+        const float x0 = RING && !ok ? __int_as_float(0x7fc00000) : kEdges || has(0) ? f[0][0] : 0.0f;
         float s[2] = {0.0f, 0.0f}, q[2] = {0.0f, 0.0f};         // two chains each
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (kEdges || has(k))
 #pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    f[k][j] -= base;
-                    s[(k * W + j) & 1] += f[k][j];
-                }
-        float sum = s[0] + s[1], c = sum * over_n;
+                for (int j = 0; j < W; ++j) s[(k * W + j) & 1] += f[k][j] - x0;
+        const float from0 = (s[0] + s[1]) * over_n, c = x0 + from0, l = (x0 - c) + from0;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (kEdges || has(k))
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
-                    const float d = may_miss(k) && !has(k) ? 0.0f : f[k][j] - c;
-                    q[(k * W + j) & 1] = fmaf(d, d, q[(k * W + j) & 1]);
+                    f[k][j] = may_miss(k) && !has(k) ? 0.0f : f[k][j] - c;
+                    q[(k * W + j) & 1] = fmaf(f[k][j], f[k][j], q[(k * W + j) & 1]);
                 }
-        float square = q[0] + q[1];
-        sum = add_lanes(sum, LANES / 2);
-        float mean = sum * over_warp, e = c - mean;
-        square = add_lanes(fmaf(n * e, e, square), LANES / 2);
+        // the warp's: mean from a reference on, the first lane's c.  q is about c, so n l^2 too large: n (e^2 - l^2) = n h (h + 2 l) comes to it with
+        // e = h + l, the distance of the thread's mean from the warp's (beyond fp32's range it stays infinite).
+        float ref = __shfl_sync(0xffffffffu, c, 0, LANES), square = q[0] + q[1];
+        float mean = add_lanes(n * ((c - ref) + l), LANES / 2) * over_warp;
+        const float h = (c - ref) - mean;
+        square = add_lanes(square > FLT_MAX ? square : fmaf(n * h, h + 2.0f * l, square), LANES / 2);
         if constexpr (OWNER != kWarp) {
-            __shared__ float2 sets[2][32];                        // taken in turn: one barrier a row is enough
+            __shared__ float4 sets[2][kMostWarps];                // mean's two parts and q; taken in turn: one barrier a row is enough
             const int lane = threadIdx.x & 31;
-            if (lane == 0) sets[turn & 1][threadIdx.x >> 5] = make_float2(sum, square);
+            float high = ref + mean;
+            if (lane == 0) sets[turn & 1][threadIdx.x >> 5] = make_float4(high, (ref - high) + mean, square, 0.0f);
             __syncthreads();
             if constexpr (RING) {
                 // everybody has the row in registers: another may come into its place
@@ -239,21 +226,25 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
                 }
                 if (++stage == stages) { stage = 0; parity ^= 1u; }
             }
-            const float2 of = lane < (int)(blockDim.x >> 5) ? sets[turn & 1][lane] : make_float2(0.0f, 0.0f);
-            sum = add_lanes(of.x, 16);
-            mean = sum * over_block;
-            e = of.x * over_lane - mean;
-            square = add_lanes(fmaf(n_lane * e, e, of.y), 16);
+            ref = sets[turn & 1][0].x;
+            const float4 of = lane < warps ? sets[turn & 1][lane] : make_float4(ref, 0.0f, 0.0f, 0.0f);
+            float from = (of.x - ref) + of.y;
+            mean = add_lanes(n_lane * from, 16) * over_block;
+            float e = from - mean;
+            square = add_lanes(fmaf(n_lane * e, e, of.z), 16);
             if constexpr (OWNER == kCluster) {
-                const float2* all = exchange.swap(make_float2(sum, square), parts, rank, turn, ok);
-                const float2 theirs = part_lane < parts ? all[part_lane] : make_float2(0.0f, 0.0f);
-                mean = add_lanes(theirs.x, kMostParts / 2) * over_p;
-                e = theirs.x * over_part - mean;
-                square = add_lanes(fmaf(n_part * e, e, theirs.y), kMostParts / 2);
+                high = ref + mean;
+                const float4* all = exchange.swap(make_float4(high, (ref - high) + mean, square, 0.0f), parts, rank, turn, ok);
+                ref = all[0].x;
+                const float4 theirs = part_lane < parts ? all[part_lane] : make_float4(ref, 0.0f, 0.0f, 0.0f);
+                from = (theirs.x - ref) + theirs.y;
+                mean = add_lanes(n_part * from, kMostParts / 2) * over_p;
+                e = from - mean;
+                square = add_lanes(fmaf(n_part * e, e, theirs.z), kMostParts / 2);
                 if (!ok) square = __int_as_float(0x7fc00000);
             }
         }
-        const float r = rsqrtf(fmaf(square, over_p, a.eps)), off = -mean * r;
+        const float r = rsqrtf(fmaf(square, over_p, a.eps)), off = ((c - ref) - mean) * r;
         auto write = [&](auto* y) {
             y += (row + ahead) * a.y_stride + at;
 #pragma unroll
@@ -283,7 +274,7 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
         else if (a.y_type == ROCKET_F16) write(static_cast<__half*>(a.y));
         else write(static_cast<__nv_bfloat16*>(a.y));
         if (first == 0 && rank == 0) {
-            if (a.mean) a.mean[row + ahead] = base + mean;
+            if (a.mean) a.mean[row + ahead] = ref + mean;
             if (a.rstd) a.rstd[row + ahead] = r;
         }
     }

@@ -75,12 +75,13 @@ __device__ __forceinline__ float add_lanes(float v, int from) {
     return v;
 }
 
-// Two values of every block of a cluster, handed to all of its blocks by stores that count on the receiver's barrier: nothing
+// Two or four values (V: float2, float4) of every block of a cluster, handed to all of its blocks by stores that count on the receiver's barrier: nothing
 // waits for the rows written meanwhile, as a cluster-wide barrier would.  One exchange per row; with two sets of buffers a block that is
 // ahead writes where nobody reads any more: it has everybody's values of the row before, sent behind the block barrier that follows
 // their reads.
+template <class V>
 struct Exchange {
-    float2 share[2][kMostParts];
+    V share[2][kMostParts];
     uint64_t bar[2];
 
     // Behind it, all blocks of the cluster must meet before the first exchange.
@@ -94,15 +95,19 @@ struct Exchange {
 
     // All threads call it with the block's value v; returns the set of buffers that holds everybody's.  turn: 0, 1, 2 ..  false in ok: a wait
     // gave up, and nothing is waited for after that.
-    __device__ __forceinline__ const float2* swap(float2 v, int parts, int rank, int turn, bool& ok) {
+    __device__ __forceinline__ const V* swap(V v, int parts, int rank, int turn, bool& ok) {
         const int set = turn & 1;
-        if (threadIdx.x == 0) fast::mbar_arrive_expect_tx(fast::smem_u32(&bar[set]), (uint32_t)(parts * sizeof(float2)));
+        if (threadIdx.x == 0) fast::mbar_arrive_expect_tx(fast::smem_u32(&bar[set]), (uint32_t)(parts * sizeof(V)));
         if ((int)threadIdx.x < parts) {
             uint32_t to, on;
             asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(fast::smem_u32(&share[set][rank])), "r"((int)threadIdx.x));
             asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(on) : "r"(fast::smem_u32(&bar[set])), "r"((int)threadIdx.x));
-            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
-                         ::"r"(to), "f"(v.x), "f"(v.y), "r"(on) : "memory");
+            if constexpr (sizeof(V) == 16)
+                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                             ::"r"(to), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(on) : "memory");
+            else
+                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                             ::"r"(to), "f"(v.x), "f"(v.y), "r"(on) : "memory");
         }
         ok = ok && wait_soon(fast::smem_u32(&bar[set]), (uint32_t)((turn >> 1) & 1));
         return share[set];
