@@ -282,7 +282,9 @@ int rocket_ridge_predict(const float* feat_dev, int N, int P, const float* w_dev
  *   gamma_dev, beta_dev  [P] of w_type, either may be NULL (1 and 0)
  *   y_dev     [N][P] of y_type, rows y_stride >= P elements apart, written; what lies between rows is not touched
  *   mean_dev, rstd_dev   [N] fp32, written where not NULL: m and 1 / sqrt(v + eps), for the backward pass
- * A row with a NaN or an infinity gives NaN in that row alone.  The statistics are fp32: a variance beyond its range gives rstd 0.  The strides count only with two rows and more.  N = 0 is a
+ * A row with a NaN or an infinity gives NaN in that row alone.  The statistics are fp32: a row with values farther than 1e18 from
+ * its mean may give rstd 0 (and y = beta), where its squares leave fp32's range; a finite row gives no NaN unless its values lie
+ * farther from one another than the largest fp32 number.  The strides count only with two rows and more.  N = 0 is a
  * successful no-op.  ROCKET_EINVAL for a NULL or misaligned pointer, N < 0, P < 1, an unknown type, a negative or non-finite
  * eps, and for an output that overlaps an input or another output (rows of two arrays may interleave at one byte distance).
  */

@@ -2,8 +2,8 @@
 //
 // Bound: memory.  A row is read once and stays in registers while its owner's next row is on its way.  A thread takes the mean of its values,
 // as c + l with l a rounding of c (from the differences to its first value, which are exact where the row is far from zero), keeps the values as
-// d = x - c, and takes the sum q of d^2.  Where sets of values meet, with n, mean and q each, the whole has the mean sum n c / sum n and
-// q = sum (q + n (c - whole's c)^2) (Chan, Golub and LeVeque); means are handed on as such pairs and added up as differences to the first set's.  So
+// d = x - c, and takes the mean square q of d.  Where sets of values meet, with a share s of the whole, mean and q each, the whole has the mean
+// sum s c and q = sum s (q + (c - whole's c)^2) (Chan, Golub and LeVeque); means are handed on as such pairs and added up as differences to the first set's.  So
 // everything is held by its distance from a mean of some of the row's values, d + (c - mean) is y's numerator, and neither a row's distance from
 // zero nor single values unlike the others cost the rest their digits; the threads of a block need one barrier, the blocks of a cluster one
 // exchange per row.
@@ -141,26 +141,26 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
             if (a.gamma && has(k)) load_typed<W>(a.gamma, a.w_type, at + k * step * W, g[k]);
             if (a.beta && has(k)) load_typed<W>(a.beta, a.w_type, at + k * step * W, b[k]);
         }
-    // values of this thread, its warp, its lane's warp, and the block
+    // Values of this thread, its warp, its lane's warp, and the block.  Sets are joined by their shares of the whole, means and mean squares, not
+    // sums, so that a row of large values leaves fp32's range only where the means themselves do.
     const int n_thread = ((words - first + step - 1) / step) * W;
     const float n = (float)(words > first ? n_thread : 0), over_n = n > 0.0f ? 1.0f / n : 0.0f;
-    const float n_warp = add_lanes(n, LANES / 2), over_warp = n_warp > 0.0f ? 1.0f / n_warp : 0.0f;
+    const float n_warp = add_lanes(n, LANES / 2), share = n_warp > 0.0f ? n / n_warp : 0.0f;
     constexpr int kMostWarps = most_threads(OWNER, WEIGHTS, NV * W) / 32;
     __shared__ float warp_n[kMostWarps];
     const int warps = blockDim.x >> 5;
-    float n_lane = 0.0f;
+    float share_warp = 0.0f;
     if constexpr (OWNER != kWarp) {
         if ((threadIdx.x & 31) == 0) warp_n[threadIdx.x >> 5] = n_warp;
         __syncthreads();
-        n_lane = (threadIdx.x & 31) < warps ? warp_n[threadIdx.x & 31] : 0.0f;
+        share_warp = (threadIdx.x & 31) < warps ? warp_n[threadIdx.x & 31] / (float)(words * W) : 0.0f;
     }
-    const float over_block = 1.0f / (float)(words * W), over_p = 1.0f / (float)a.P;
     // the cluster's blocks, a lane for each in both halves of a warp
     const int part_lane = threadIdx.x & (kMostParts - 1);
-    float n_part = 0.0f;
+    float share_part = 0.0f;
     if (OWNER == kCluster && part_lane < parts) {
         const int64_t all = a.P / W;
-        n_part = (float)(((int)(all * (part_lane + 1) / parts) - (int)(all * part_lane / parts)) * W);
+        share_part = (float)(((int)(all * (part_lane + 1) / parts) - (int)(all * part_lane / parts)) * W) / (float)a.P;
     }
     if constexpr (OWNER == kCluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     bool ok = true;
@@ -196,8 +196,8 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
         for (int k = 0; k < NV; ++k)
             if (kEdges || has(k))
 #pragma unroll
-                for (int j = 0; j < W; ++j) s[(k * W + j) & 1] += f[k][j] - x0;
-        const float from0 = (s[0] + s[1]) * over_n, c = x0 + from0, l = (x0 - c) + from0;
+                for (int j = 0; j < W; ++j) s[(k * W + j) & 1] = fmaf(f[k][j] - x0, over_n, s[(k * W + j) & 1]);
+        const float from0 = s[0] + s[1], c = x0 + from0, l = (x0 - c) + from0;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (kEdges || has(k))
@@ -206,14 +206,14 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
                     f[k][j] = may_miss(k) && !has(k) ? 0.0f : f[k][j] - c;
                     q[(k * W + j) & 1] = fmaf(f[k][j], f[k][j], q[(k * W + j) & 1]);
                 }
-        // the warp's: mean from a reference on, the first lane's c.  q is about c, so n l^2 too large: n (e^2 - l^2) = n h (h + 2 l) comes to it with
+        // the warp's: mean from a reference on, the first lane's c.  q / n is about c, so l^2 too large: e^2 - l^2 = h (h + 2 l) comes to it with
         // e = h + l, the distance of the thread's mean from the warp's (beyond fp32's range it stays infinite).
-        float ref = __shfl_sync(0xffffffffu, c, 0, LANES), square = q[0] + q[1];
-        float mean = add_lanes(n * ((c - ref) + l), LANES / 2) * over_warp;
+        float ref = __shfl_sync(0xffffffffu, c, 0, LANES), square = (q[0] + q[1]) * over_n;
+        float mean = add_lanes(share * ((c - ref) + l), LANES / 2);
         const float h = (c - ref) - mean;
-        square = add_lanes(square > FLT_MAX ? square : fmaf(n * h, h + 2.0f * l, square), LANES / 2);
+        square = add_lanes(square > FLT_MAX ? square : fmaf(share * h, h + 2.0f * l, share * square), LANES / 2);
         if constexpr (OWNER != kWarp) {
-            __shared__ float4 sets[2][kMostWarps];                // mean's two parts and q; taken in turn: one barrier a row is enough
+            __shared__ float4 sets[2][kMostWarps];                // mean's two parts and the mean square; taken in turn: one barrier a row is enough
             const int lane = threadIdx.x & 31;
             float high = ref + mean;
             if (lane == 0) sets[turn & 1][threadIdx.x >> 5] = make_float4(high, (ref - high) + mean, square, 0.0f);
@@ -229,22 +229,22 @@ rows_kernel(const Forward a, int parts, int stages, int stage_words) {
             ref = sets[turn & 1][0].x;
             const float4 of = lane < warps ? sets[turn & 1][lane] : make_float4(ref, 0.0f, 0.0f, 0.0f);
             float from = (of.x - ref) + of.y;
-            mean = add_lanes(n_lane * from, 16) * over_block;
+            mean = add_lanes(share_warp * from, 16);
             float e = from - mean;
-            square = add_lanes(fmaf(n_lane * e, e, of.z), 16);
+            square = add_lanes(fmaf(share_warp * e, e, share_warp * of.z), 16);
             if constexpr (OWNER == kCluster) {
                 high = ref + mean;
                 const float4* all = exchange.swap(make_float4(high, (ref - high) + mean, square, 0.0f), parts, rank, turn, ok);
                 ref = all[0].x;
                 const float4 theirs = part_lane < parts ? all[part_lane] : make_float4(ref, 0.0f, 0.0f, 0.0f);
                 from = (theirs.x - ref) + theirs.y;
-                mean = add_lanes(n_part * from, kMostParts / 2) * over_p;
+                mean = add_lanes(share_part * from, kMostParts / 2);
                 e = from - mean;
-                square = add_lanes(fmaf(n_part * e, e, theirs.z), kMostParts / 2);
+                square = add_lanes(fmaf(share_part * e, e, share_part * theirs.z), kMostParts / 2);
                 if (!ok) square = __int_as_float(0x7fc00000);
             }
         }
-        const float r = rsqrtf(fmaf(square, over_p, a.eps)), off = ((c - ref) - mean) * r;
+        const float r = rsqrtf(square + a.eps), off = ((c - ref) - mean) * r;
         auto write = [&](auto* y) {
             y += (row + ahead) * a.y_stride + at;
 #pragma unroll

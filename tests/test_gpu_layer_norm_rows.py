@@ -15,6 +15,8 @@ from test_gpu_layer_norm import EPS, _check_forward, _torch, _type, _vec
 
 pytestmark = pytest.mark.gpu
 
+U = 2.0 ** -24
+
 # what is put where, on rows N(loc, 1)
 ROWS = {
     "first three large": (0.0, lambda x: x.__setitem__((slice(None), slice(0, 3)), 100.0 + x[:, :3])),
@@ -49,5 +51,37 @@ def test_values_unlike_the_rest_in_many_rows(N, P, kind):
     loc, put = ROWS[kind]
     feat = loc + torch.randn((N, P), generator=gen, device="cuda")
     put(feat)
+    out, mean, rstd = rk.rocket_layer_norm(feat)
+    _check_forward(feat, None, None, EPS, out, mean, rstd)
+
+
+@pytest.mark.parametrize("P", [2, 40, 257, 1500, 2049, 4096, 20000, 20003, 81000, 131072, 320000, 400001])
+@pytest.mark.parametrize("low,high", [(1e35, 3e35), (1e37, 3e37), (-1e38, 2e38), (2e38, 3.4e38), (-3.4e38, -3.3e38)])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_finite_rows_at_the_ends_of_the_range(x, low, high, P):
+    torch = _torch()
+    rng = np.random.default_rng(P)
+    feat = torch.from_numpy(rng.uniform(low, high, size=(3, P))).to(_type(x)).cuda()
+    if x == "bf16":
+        feat = feat.clamp(-3.38e38, 3.38e38)
+    assert bool(torch.isfinite(feat).all())
+    g, b = _vec(rng, P, torch.float32, 1.0), _vec(rng, P, torch.float32, 0.0)
+    out, mean, rstd = rk.rocket_layer_norm(feat, g, b, EPS, out_dtype=torch.float32)
+    v = feat.double()
+    m, s = v.mean(1), v.std(1, correction=0)
+    assert bool(((mean.double() - m).abs() <= 2 * U * m.abs() + 80 * U * s).all())
+    zero = rstd == 0
+    # 1 / s where doubles sum up the squares (and fp32 still holds it to half a step, 2^-150 where it is subnormal)
+    assert bool((zero | ((rstd.double() - 1 / s).abs() <= 48 * U / s + 2.0 ** -149)).all())
+    assert torch.equal(out[zero], b.expand(3, P)[zero])
+    assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("P", [40, 1500, 4096, 20000, 20003, 131072, 320000, 400001])
+def test_variances_whose_sums_leave_single_precision(P):
+    # values within 1e18 of the mean: squares up to 1e36, sums of them up to 3e40
+    torch = _torch()
+    rng = np.random.default_rng(P)
+    feat = torch.from_numpy((2e17 * np.clip(rng.normal(size=(3, P)), -4.9, 4.9)).astype(np.float32)).cuda()
     out, mean, rstd = rk.rocket_layer_norm(feat)
     _check_forward(feat, None, None, EPS, out, mean, rstd)
