@@ -48,17 +48,18 @@ __global__ void __launch_bounds__(WARPS * 32) sum_owners_kernel(const float* __r
 }  // namespace
 
 int64_t backward_workspace(int N, int P) {
-    const int owners = owners_of(N, P);
+    const int owners = owners_of(N, P, true);
     return owners > 1 && !is_joined(N, P) ? (int64_t)owners * 2 * P * (int64_t)sizeof(float) : 0;
 }
 
 cudaError_t launch_backward(const Backward& args, cudaStream_t stream) {
     Backward a = args;
     if (a.N == 0 && !a.dgamma && !a.dbeta) return cudaSuccess;
-    a.joined = (a.dgamma || a.dbeta) && is_joined(a.N, a.P);
-    int owners = owners_of(a.N, a.P);
+    const bool weights = a.dgamma || a.dbeta;
+    a.joined = weights && is_joined(a.N, a.P);
+    int owners = owners_of(a.N, a.P, weights);
     const cudaError_t e = with_float_type(a.x_type, [&](auto* px) { return launch_rows<std::remove_pointer_t<decltype(px)>>(a, owners, stream); });
-    if (e != cudaSuccess || owners <= 1 || a.joined || (!a.dgamma && !a.dbeta)) return e;
+    if (e != cudaSuccess || owners <= 1 || a.joined || !weights) return e;
     auto sum = [&](auto kernel, int columns, int warps) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)((a.P + columns - 1) / columns));

@@ -72,3 +72,16 @@ def test_one_of_the_sums_of_few_rows(N, P):
         assert dg is None and torch.equal(db, wb)
         _, dg, db = rk.rocket_layer_norm_backward(dy, feat, *_unit(N))
         assert torch.equal(dg, wg) and torch.equal(db, wb)
+
+
+@pytest.mark.parametrize("N,P", [(1, 5), (4, 1000), (20, 1000), (128, 1001), (128, 4096), (64, 4095), (4096, 128), (4097, 128), (2048, 256), (1024, 512), (1, 20000), (3, 20000)])
+@pytest.mark.parametrize("x,y", [("f32", "f32"), ("bf16", "bf16")])
+def test_dx_alone_has_the_bits_of_dx_with_the_sums(N, P, x, y):
+    torch = _torch()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N)
+    feat, dy = _whole(gen, N, P, _type(x), 0, 0, 3), _whole(gen, N, P, _type(y), 0, 0, 3)
+    dx, dg, db = rk.rocket_layer_norm_backward(dy, feat, *_unit(N), want_weights=False)
+    assert dg is None and db is None
+    _check_dx(dx, dy, feat)
+    assert torch.equal(dx, rk.rocket_layer_norm_backward(dy, feat, *_unit(N))[0])
