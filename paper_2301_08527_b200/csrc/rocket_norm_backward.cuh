@@ -85,7 +85,8 @@ __device__ __forceinline__ float2 row_sums(float2 v, int turn) {
     return make_float2(__shfl_sync(0xffffffffu, s, 0), __shfl_sync(0xffffffffu, s, 16));
 }
 
-// dg and db from the sums [2][P] that every block of a cluster has in shared memory: each block adds up a share of the columns, in the blocks' order.
+// dg and db from the sums [2][P] that every block of a cluster has in shared memory: each block adds up a share of the columns, in the blocks' order, in
+// double precision.
 __device__ __forceinline__ void join_owners(const float* sums, const Backward& a) {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -93,14 +94,15 @@ __device__ __forceinline__ void join_owners(const float* sums, const Backward& a
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < 2 * a.P; i += blocks * blockDim.x) {
         void* out = i < a.P ? a.dgamma : a.dbeta;
         if (!out) continue;
-        float v[1] = {0.0f};
+        double sum = 0.0;
         for (int b = 0; b < blocks; ++b) {
             uint32_t from;
             float x;
             asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(fast::smem_u32(sums + i)), "r"(b));
             asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(from) : "memory");
-            v[0] += x;
+            sum += (double)x;
         }
+        const float v[1] = {(float)sum};
         store_typed<1>(out, a.w_type, i < a.P ? i : i - a.P, v);
     }
     // no block ends while another still reads its sums: the arrival stands behind the reads

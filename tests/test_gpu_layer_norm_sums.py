@@ -85,3 +85,40 @@ def test_dx_alone_has_the_bits_of_dx_with_the_sums(N, P, x, y):
     assert dg is None and db is None
     _check_dx(dx, dy, feat)
     assert torch.equal(dx, rk.rocket_layer_norm_backward(dy, feat, *_unit(N))[0])
+
+
+def _check_whole_sums(N, P, x, y, at, pad, low, most):
+    """dgamma and dbeta to the bit: sums over up to an eighth of the rows stay below 2^24 and are exact in fp32, the whole's are rounded to fp32 once."""
+    torch = _torch()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N + P)
+    feat, dy = _whole(gen, N, P, _type(x), at, pad, 2), _whole(gen, N, P, _type(y), at, pad, most)
+    if low is not None:                         # of one sign
+        feat.copy_(feat.abs() + 1)
+        dy.copy_(dy.abs().clamp(min=low))
+    dx, dg, db = rk.rocket_layer_norm_backward(dy, feat, *_unit(N))
+    # whole sums of up to 2^53: exact in double, by columns to spare memory
+    for lo in range(0, P, 256):
+        d, v = dy[:, lo:lo + 256].double(), feat[:, lo:lo + 256].double()
+        assert torch.equal(dg[lo:lo + 256], (d * v).sum(0).float()) and torch.equal(db[lo:lo + 256], d.sum(0).float())
+    return dx, dy, feat
+
+
+# one row and more above what 16 blocks join, for 8, 16 and 32 lanes and for blocks and clusters; on and off 16-byte borders: words of 8, 4 and 1
+ABOVE = [(4097, 64), (4111, 128), (5000, 100), (4999, 97), (2049, 136), (2500, 200), (2499, 256), (2100, 251), (1025, 264), (1500, 320), (1499, 512), (1100, 505), (129, 520),
+         (300, 1000), (299, 1001), (150, 4096), (20, 4104), (400, 9996), (77, 20000), (40, 33001)]
+
+
+@pytest.mark.parametrize("N,P", ABOVE + [(4096, 128), (2048, 256), (1024, 512), (128, 4096), (3000, 96), (500, 300), (100, 1003)])
+@pytest.mark.parametrize("x,y", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("at,pad", [(0, 0), (1, 0), (0, 8)])
+def test_every_row_counts_once(N, P, x, y, at, pad):
+    dx, dy, feat = _check_whole_sums(N, P, x, y, at, pad, None, 3)
+    _check_dx(dx, dy, feat)
+
+
+@pytest.mark.parametrize("N,P", [(70001, 64), (50000, 200), (40001, 257), (30000, 512), (20000, 1000), (12000, 4096), (12001, 4099), (8000, 9996), (4096, 128), (2000, 256), (128, 4096)])
+def test_long_sums_of_one_sign_are_rounded_once(N, P):
+    # dy of about 3/4 of most and x of 2.2 in the mean: sums of about 2^26, 1.65 most N, of which an eighth is below 2^24
+    most = int(2 ** 26 / (1.65 * N))
+    _check_whole_sums(N, P, "f32", "f32", 0, 0, most // 2, most)
