@@ -607,6 +607,13 @@ def _dense(t):
     return True
 
 
+def _same_order(a, b):
+    """Whether two dense tensors of one size hold their values in the same order (the stride of a single value tells nothing)."""
+    if a.is_contiguous() and b.is_contiguous():
+        return True
+    return a.shape == b.shape and all(n <= 1 or s == t for n, s, t in zip(a.shape, a.stride(), b.stride()))
+
+
 def _tensor_list(ts, name):
     """(count, addresses, sizes, type codes, device number, all contiguous) of a sequence of CUDA tensors, as arrays.  Long lists are the
     rule, so every property is asked for in one sweep."""
@@ -644,8 +651,7 @@ def _norm_call(grads, max_norm, out, norm_out):
         m, outs, out_sizes, out_codes, out_device, out_contiguous = _tensor_list(out, "out")
         if m != n or out_sizes != sizes or out_device != device:
             raise ValueError("out must hold one tensor per gradient, of its size, on the same device")
-        if not (contiguous and out_contiguous) and any(
-                a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
+        if not (contiguous and out_contiguous) and not all(map(_same_order, grads, out)):
             raise ValueError("out must have the shapes and strides of the gradients")
     if n == 0:
         device = norm_out.get_device() if isinstance(norm_out, torch.Tensor) and norm_out.is_cuda else _current_device()
