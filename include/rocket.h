@@ -284,7 +284,7 @@ int rocket_ridge_predict(const float* feat_dev, int N, int P, const float* w_dev
  *   mean_dev, rstd_dev   [N] fp32, written where not NULL: m and 1 / sqrt(v + eps), for the backward pass
  * A row with a NaN or an infinity gives NaN in that row alone.  The statistics are fp32: a row with values farther than 1e18 from
  * its mean may give rstd 0 (and y = beta), where its squares leave fp32's range; a finite row gives no NaN unless its values lie
- * farther from one another than the largest fp32 number.  The strides count only with two rows and more.  N = 0 is a
+ * farther from one another than the largest fp32 number, or are all equal with eps 0.  The strides count only with two rows and more.  N = 0 is a
  * successful no-op.  ROCKET_EINVAL for a NULL or misaligned pointer, N < 0, P < 1, an unknown type, a negative or non-finite
  * eps, and for an output that overlaps an input or another output (rows of two arrays may interleave at one byte distance).
  */
@@ -321,7 +321,8 @@ int rocket_layer_norm_backward(const void* dy_dev, int y_type, int64_t dy_stride
  *   workspace_dev  workspace_bytes >= rocket_grad_norm_workspace(count, sizes) (ROCKET_EINVAL for sizes out of range); NULL is
  *              allowed where that is 0, as it is for a small gradient in few tensors
  * Squares and sums are taken in double precision: no finite gradient overflows or vanishes in them.  The same call gives the
- * same bits each time.  An infinite norm gives c = 0 (for max_norm finite), a NaN gives NaN everywhere; a caller that would
+ * same bits each time.  norm and c are fp32: a c below 1e-38 has fewer digits, and a norm beyond 3.4e38 is infinite, which gives
+ * c = 0 (for max_norm finite), a NaN gives NaN everywhere; a caller that would
  * rather skip such a step reads norm_dev.  ROCKET_EINVAL for a NULL or misaligned pointer, a negative count or size, an unknown or
  * unfitting type, max_norm negative or NaN, and where anything written overlaps anything else (one tensor listed twice can be
  * measured, not clipped).

@@ -8,7 +8,7 @@
 // A block's rows come into shared memory by bulk copies, several rows ahead (a warp's, which are short, are loaded by its lanes).
 // Every wait is bounded; a thread that gives up counts as NaN, which makes the row's dx and the thread's sums NaN.
 //
-// Measured with the second kernel: 16,384 x 4,096 bf16 78 us, 5.2 TB/s or 80 % of a copy (1,135 with a pass per output); 677 x 9,996 fp32 and bf16
+// Measured with the second kernel: 16,384 x 4,096 bf16 79 us, 5.1 TB/s or 79 % of a copy (1,135 with a pass per output); 677 x 9,996 fp32 and bf16
 // 28 us (43 with more clusters than run at once, 31 with a cluster barrier per row); 8,000 x 2,001 fp32 41 us, where loads by the threads took 150.
 #pragma once
 
@@ -22,7 +22,10 @@ namespace rocket {
 namespace norm {
 
 constexpr int kColumns = 16;              // of a thread
-constexpr int kThreads = 256;             // most of a block; 128 registers each, so that 512 threads share an SM
+// Most of a block.  Rows of blocks and clusters: 128 registers each, so that 512 threads share an SM.  Short rows: as many as they ask for, up to 184;
+// above 128 an SM has one block of the two that the grid counts on, and the grid runs in two rounds.  Cut to 128, 100,000 x 256 fp32 takes 68 us for
+// 59 and 100,000 x 255 bf16 154 for 57 (60,000 x 512 fp32 64 for 70).
+constexpr int kThreads = 256;
 constexpr int kMostStages = 8;
 constexpr int kWarpColumns = 32 * kColumns;
 constexpr int kSmemSm = 227 * 1024;       // shared memory of an SM
@@ -51,8 +54,9 @@ inline bool is_long(int P) { return parts_of(P) > kMostParts; }
 // Rows that a block has at a time.
 inline int block_rows(int P) { return is_short(P) ? kThreads / lanes_of(P) : 1; }
 // Few rows: the blocks of one cluster are all owners, and add their sums up in distributed shared memory: no workspace, and no second launch.
-// Up to so many turns of each: 32 rows of 1,000 columns take 4.6 us of device time so and 4.0 with a second kernel, 128 rows 8.5 and 4.3, but that kernel's
-// launch and workspace cost the caller 4.3.
+// Up to so many turns of each.  A call costs 15 us so and 19 with a second kernel, its launch and its workspace, at every length; the device's own time,
+// which counts in captured graphs, is 4.8 us so and 3.9 by a second kernel for 32 x 1,000 fp32, 8.6 and 4.1 for 128 x 1,000, 10.9 and 6.8 for
+// 128 x 4,096, 8.7 and 4.8 for 4,096 x 128, and 14 and 5.3 at most (128 x 1,001).
 constexpr int kJoinedTurns = 8;
 inline bool is_joined(int N, int P) { return parts_of(P) == 1 && N <= (int64_t)kMostParts * block_rows(P) * kJoinedTurns; }
 

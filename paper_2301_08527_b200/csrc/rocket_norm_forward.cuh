@@ -12,7 +12,7 @@
 // registers.  The owners stay and go through the rows in turn.
 //
 // Measured: 16,384 x 4,096 bf16 50 us, 5.4 TB/s or 83 % of a copy (56 with two barriers a row and 16 values a thread, whose sums then are a third of the
-// instructions; 79 with a block per row and no rows ahead); 677 x 20,000 fp32 to bf16 20 us (28 with a block of 1,024 threads per row that fetches gamma
+// instructions; 79 with a block per row and no rows ahead); 677 x 20,000 fp32 to bf16 18 us (28 with a block of 1,024 threads per row that fetches gamma
 // and beta again for each).
 #pragma once
 
@@ -419,7 +419,7 @@ cudaError_t launch_words(const Forward& a, cudaStream_t stream) {
     if (a.P > 1 << 20) return launch_long<T>(a, stream);            // more than any cluster's registers hold; sums of sizes below fit into 32 bits
     const int words = a.P / W;
     // Short rows: as few lanes of a warp as hold the row in up to 16 values each (up to 20 in 16 lanes, 32 in 32), since half of a warp's work
-    // would else be the sums' shuffles: 100,003 rows of 257 binary16 values take 28 us with 16 lanes and 31 with 32.
+    // would else be the sums' shuffles: 100,003 rows of 257 binary16 values take 27 us with 16 lanes; with 32 they took 3 more.
     constexpr int kMost = W == 1 ? 16 : 32 / W, kFew = 16 / W, kMiddle = W == 1 ? 20 : 16 / W;
     if (words <= 8 * kFew)
         return with_int<1, kFew>((words + 7) / 8, [&](auto nv) { return launch<T, W, nv.value, kWarp, kHold, kLast, 8>(a, 256, 1, stream); });
@@ -430,7 +430,8 @@ cudaError_t launch_words(const Forward& a, cudaStream_t stream) {
             return launch<T, W, nv.value, kWarp, nv.value * W <= 16 ? kHold : kAsk, kLast>(a, 256, 1, stream);
         });
     // Enough rows, or none of whose words is of 16 bytes: gamma and beta stay in registers, in a block where they fit, else in a cluster
-    // (677 x 20,000 20 us so and 25 with blocks that load them for every row; 8,000 x 2,001 27 us so and 56).
+    // (677 x 20,000 20 us so and 25 with blocks that load them for every row; 8,000 x 2,001 27 us so and 56).  Two thirds of the odd lengths from 513 to
+    // 4,095 have threads that miss more than their last word (kAny) and gain nothing so: 8,736 x 2,049 53 us.
     constexpr int kHeld = held_values(W) / W, kThreads = hold_threads(kBlock, held_values(W)), kPartThreads = hold_threads(kCluster, held_values(W));
     constexpr int kAtOnce = W == 1 ? 768 : 512;                      // threads of an SM, by the registers they are given
     constexpr bool kWide = W * sizeof(T) == 16;                      // every row begins and ends on a 16-byte border
